@@ -284,6 +284,50 @@ int tsa_layer_drift(const void* h_in, const void* h_out, int64_t n_tokens, int32
  *   drift [n_layers] fp32, host;  is_sparse [n_layers] int32, host, out (1 = apply Token Sparse Attention). */
 int tsa_sparse_layers(const float* drift, int32_t n_layers, double delta, int32_t* is_sparse);
 
+/* Rotary positions on Q and K, the step before scoring and attention (Q, K arrive position-encoded there).
+ * Row (b, h, t) at position p = positions[b * L + t] (device int32 [B,L], any value), or start + t where positions is
+ * NULL; the pair (x, y) of its columns that belongs to freq[i] becomes
+ *   gain * (x cos a - y sin a, x sin a + y cos a),  a = p * freq[i],   i = 0 .. rot / 2 - 1.
+ * Columns rot .. d - 1 are copied.  bf16 in and out, fp32 arithmetic, one rounding; angles are exact to 2^-32 of a turn
+ * at every position.  A packed batch of sequences is B = 1, L = all tokens, with positions. */
+#define TSA_ROTARY_MAX_FREQS 64
+typedef struct tsa_rotary_desc {
+  int32_t B, Hq, Hkv, L;    /* as in tsa_desc; L = 0: nothing to do */
+  int32_t d;                /* 64 or 128 */
+  int32_t rot;              /* columns that are rotated, the first ones: a multiple of 16, at most d */
+  int32_t interleaved;      /* 0: column i and column i + rot / 2 are a pair; 1: columns 2 i and 2 i + 1 */
+  int32_t start;
+  float gain;               /* factor on the rotated columns; 0 means 1 */
+  int32_t reserved;         /* 0 */
+  /* element strides of Q [B,Hq,L,d], K [B,Hkv,L,d] and of their rotated copies, as in tsa_desc: all three of a tensor 0
+   * means contiguous; multiples of 8, stride_l >= d */
+  int64_t q_stride_b, q_stride_h, q_stride_l;
+  int64_t k_stride_b, k_stride_h, k_stride_l;
+  int64_t q_out_stride_b, q_out_stride_h, q_out_stride_l;
+  int64_t k_out_stride_b, k_out_stride_h, k_out_stride_l;
+  double freq[TSA_ROTARY_MAX_FREQS];   /* radians per position of pair i; the first rot / 2 are used */
+} tsa_rotary_desc;
+
+/* Q -> Q_out, K -> K_out; either pair may be NULL (both of it).  An output may be its input (same pointer and strides); any
+ * other overlap is not allowed. */
+int tsa_rotary(const tsa_rotary_desc* desc, const void* Q, const void* K, const int32_t* positions,
+               void* Q_out, void* K_out, void* stream);
+
+/* The frequencies on the HOST: freq[i] = base^(-2 i / rot), i < rot / 2, stretched for contexts `factor` times as long as the
+ * `original` length:
+ *   TSA_ROTARY_PLAIN       as they are (factor and original are not used)
+ *   TSA_ROTARY_LINEAR      freq / factor
+ *   TSA_ROTARY_BASE        base * factor^(rot / (rot - 2)) in place of base
+ *   TSA_ROTARY_PARTS       by how often a pair turns within the original length: pairs that turn more than `high` times stay,
+ *                          those below `low` turns become freq / factor, between them linear in the pair's index (bounds of
+ *                          the ramp rounded outwards to whole indices); *gain = 0.1 ln(factor) + 1
+ *   TSA_ROTARY_WAVELENGTH  the same idea, linear in the number of turns between `low` and `high`
+ * *gain is 1 otherwise.  high and low: 0, 0 means 32, 1 for PARTS and 4, 1 for WAVELENGTH.
+ * freq: rot / 2 doubles out;  gain: out. */
+enum { TSA_ROTARY_PLAIN = 0, TSA_ROTARY_LINEAR = 1, TSA_ROTARY_BASE = 2, TSA_ROTARY_PARTS = 3, TSA_ROTARY_WAVELENGTH = 4 };
+int tsa_rotary_frequencies(int32_t kind, int32_t rot, double base, double factor, double original, double high, double low,
+                           double* freq, float* gain);
+
 #ifdef __cplusplus
 }
 #endif

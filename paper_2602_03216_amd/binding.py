@@ -19,7 +19,10 @@ EXPORTS = ("tsa_version", "tsa_last_error", "tsa_keep_count", "tsa_workspace_byt
            "tsa_select", "tsa_compress", "tsa_attend_workspace_bytes", "tsa_attend", "tsa_decompress", "tsa_compress_v_tiles", "tsa_attend_fused", "tsa_forward",
            "tsa_forward_dynamic_workspace_bytes", "tsa_forward_dynamic",
            "tsa_layer_drift_workspace_bytes", "tsa_layer_drift", "tsa_sparse_layers", "tsa_mfma_probe", "tsa_mix_probe", "tsa_read_probe", "tsa_copy_probe", "tsa_bench_set_attend_form",
-           "tsa_select_static", "tsa_select_static_capacity")
+           "tsa_select_static", "tsa_select_static_capacity", "tsa_rotary", "tsa_rotary_frequencies")
+
+TSA_ROTARY_MAX_FREQS = 64
+TSA_ROTARY_PLAIN, TSA_ROTARY_LINEAR, TSA_ROTARY_BASE, TSA_ROTARY_PARTS, TSA_ROTARY_WAVELENGTH = 0, 1, 2, 3, 4
 
 
 class TsaError(RuntimeError):
@@ -47,6 +50,22 @@ def make_desc(B, Hq, Hkv, L, d, last_q=64, pool_w=1, group_mode=0, force_first=0
 def blhd_strides(H, L, d):
     """Strides of a [B,L,H,d] tensor addressed as (b, h, t)."""
     return (L * H * d, d, H * d)
+
+
+class tsa_rotary_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "L", "d", "rot", "interleaved", "start")] + \
+               [("gain", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [("%s_stride_%s" % (t, a), ctypes.c_int64) for t in ("q", "k", "q_out", "k_out") for a in "bhl"] + \
+               [("freq", ctypes.c_double * TSA_ROTARY_MAX_FREQS)]
+
+
+def make_rotary_desc(B, Hq, Hkv, L, d, freq, interleaved=0, start=0, gain=1.0, q_strides=(0, 0, 0), k_strides=(0, 0, 0),
+                     q_out_strides=(0, 0, 0), k_out_strides=(0, 0, 0)):
+    """freq: radians per position of every pair (rot = 2 len(freq) columns are rotated); strides as in make_desc."""
+    if len(freq) > TSA_ROTARY_MAX_FREQS:
+        raise TsaError(TSA_ERR_ARG, "at most %d frequencies" % TSA_ROTARY_MAX_FREQS)
+    return tsa_rotary_desc(B, Hq, Hkv, L, d, 2 * len(freq), interleaved, start, gain, 0, *q_strides, *k_strides, *q_out_strides,
+                           *k_out_strides, (ctypes.c_double * TSA_ROTARY_MAX_FREQS)(*[float(f) for f in freq]))
 
 
 _lib = None
@@ -128,6 +147,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.tsa_layer_drift.argtypes = [vp, vp, ctypes.c_int64, i32, ctypes.c_float, vp, vp, sz, vp]
     lib.tsa_sparse_layers.restype = ctypes.c_int
     lib.tsa_sparse_layers.argtypes = [ctypes.POINTER(ctypes.c_float), i32, ctypes.c_double, ctypes.POINTER(i32)]
+    lib.tsa_rotary.restype = ctypes.c_int
+    lib.tsa_rotary.argtypes = [ctypes.POINTER(tsa_rotary_desc), vp, vp, vp, vp, vp, vp]
+    dbl = ctypes.c_double
+    lib.tsa_rotary_frequencies.restype = ctypes.c_int
+    lib.tsa_rotary_frequencies.argtypes = [i32, i32, dbl, dbl, dbl, dbl, dbl, ctypes.POINTER(dbl), ctypes.POINTER(ctypes.c_float)]
     _lib = lib
     return lib
 
@@ -297,6 +321,41 @@ def tsa_sparse_layers(drift, delta=0.5):
     out = (ctypes.c_int32 * n)()
     _check(load_library().tsa_sparse_layers(arr, n, float(delta), out))
     return list(out)
+
+
+def _view(t, dtype, shape, name, strides=None):
+    """Address of a tensor that has to be of this type and shape.  strides: element strides of all axes but the last, as the descriptor
+    has them (zeros: contiguous); the tensor's own have to be the same."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise TsaError(TSA_ERR_ARG, "%s is not on the current GPU" % name)
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise TsaError(TSA_ERR_ARG, "%s is %s" % (name, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise TsaError(TSA_ERR_ARG, "%s is %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    if strides is None or not any(strides):
+        if not t.is_contiguous():
+            raise TsaError(TSA_ERR_ARG, "%s is not contiguous" % name)
+    elif any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), (*strides, 1))):
+        raise TsaError(TSA_ERR_ARG, "%s has strides %s, the descriptor %s" % (name, t.stride(), tuple(strides)))
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def tsa_rotary_frequencies(kind, rot, base, factor=1.0, original=0.0, high=0.0, low=0.0):
+    """(frequencies, gain) for make_rotary_desc."""
+    freq, gain = (ctypes.c_double * max(1, rot // 2))(), ctypes.c_float()
+    _check(load_library().tsa_rotary_frequencies(kind, rot, base, factor, original, high, low, freq, ctypes.byref(gain)))
+    return list(freq), gain.value
+
+
+def tsa_rotary(desc, Q, K, Q_out, K_out, positions=None):
+    """Q [B,Hq,L,d], K [B,Hkv,L,d] and their outputs: bf16 tensors or views with the descriptor's strides; positions int32 [B,L]."""
+    def at(t, heads, which, name):
+        return _view(t, torch.bfloat16, (desc.B, heads, desc.L, desc.d), name, [getattr(desc, "%s_stride_%s" % (which, x)) for x in "bhl"])
+    _check(load_library().tsa_rotary(ctypes.byref(desc), at(Q, desc.Hq, "q", "Q"), at(K, desc.Hkv, "k", "K"),
+                                     _view(positions, torch.int32, (desc.B, desc.L), "positions"),
+                                     at(Q_out, desc.Hq, "q_out", "Q_out"), at(K_out, desc.Hkv, "k_out", "K_out"), _stream()))
 
 
 def tsa_mfma_probe(operands, iters, blocks, sink, clocks):

@@ -507,6 +507,107 @@ int tsa_sparse_layers(const float* drift, int32_t n_layers, double delta, int32_
   return TSA_OK;
 }
 
+namespace {
+
+// Layout of a [B,heads,L,d] tensor as the caller gives it (all three 0: contiguous); strides of axes of length 1 are not used.
+int check_layout(const char* name, int64_t b, int64_t h, int64_t l, int64_t B, int64_t heads, int64_t L, int64_t d, tsa::Strides* out) {
+  if (b == 0 && h == 0 && l == 0) {
+    *out = tsa::Strides{(long long)(heads * L * d), (long long)(L * d), (long long)d};
+    return TSA_OK;
+  }
+  if (B == 1) b = 0;
+  if (heads == 1) h = 0;
+  if (L == 1) l = d;
+  if (b < 0 || h < 0 || l < d || (b | h | l) % 8 != 0)
+    return fail(TSA_ERR_ARG, "%s strides: multiples of 8 elements, the row stride >= d, none negative (or all 0)", name);
+  if ((B > 1 && b == 0) || (heads > 1 && h == 0)) return fail(TSA_ERR_ARG, "a %s stride is 0", name);
+  const int64_t most = (int64_t)1 << 46;                 // offsets stay far inside 64 bits
+  if (b > most || h > most || l > most) return fail(TSA_ERR_UNSUPPORTED, "%s strides must stay below 2^46 elements", name);
+  *out = tsa::Strides{(long long)b, (long long)h, (long long)l};
+  return TSA_OK;
+}
+
+}  // namespace
+
+int tsa_rotary(const tsa_rotary_desc* d, const void* Q, const void* K, const int32_t* positions, void* Q_out, void* K_out, void* stream) {
+  int rc;
+  if (!d) return fail(TSA_ERR_ARG, "desc is NULL");
+  if (d->B < 1 || d->L < 0) return fail(TSA_ERR_ARG, "B must be >= 1 and L >= 0");
+  if ((long long)d->B * d->L > 0x7fffffffLL) return fail(TSA_ERR_UNSUPPORTED, "B * L above 2^31 - 1");
+  if (d->d != 64 && d->d != 128) return fail(TSA_ERR_UNSUPPORTED, "head dimension %d: only 64 and 128 are built", d->d);
+  if (d->rot < 16 || d->rot > d->d || d->rot % 16 != 0) return fail(TSA_ERR_UNSUPPORTED, "rot (%d) must be a multiple of 16 in [16, d]", d->rot);
+  if (d->interleaved != 0 && d->interleaved != 1) return fail(TSA_ERR_ARG, "interleaved must be 0 or 1");
+  if (d->reserved != 0) return fail(TSA_ERR_ARG, "reserved must be 0");
+  if (d->L == 0) return TSA_OK;
+  if (!std::isfinite(d->gain)) return fail(TSA_ERR_ARG, "gain must be finite");
+  if (!positions && (long long)d->start + d->L > 0x7fffffffLL) return fail(TSA_ERR_ARG, "start + L passes 2^31 - 1");
+  if (((uintptr_t)positions & 3u) != 0) return fail(TSA_ERR_ARG, "positions is not 4-byte aligned");
+  if (!Q != !Q_out || !K != !K_out || (!Q && !K)) return fail(TSA_ERR_ARG, "Q with Q_out, K with K_out, and one pair at least");
+  tsa::RotaryArgs a;
+  a.Q = Q; a.K = K; a.Qo = Q_out; a.Ko = K_out; a.positions = positions;
+  a.B = d->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.L = d->L; a.d = d->d; a.rot = d->rot; a.interleaved = d->interleaved; a.start = d->start;
+  a.gain = d->gain == 0.0f ? 1.0f : d->gain;
+  a.q = a.k = a.qo = a.ko = tsa::Strides{0, 0, 0};
+  struct { const char* name; const void* in; const void* out; int heads; const int64_t* si; const int64_t* so; tsa::Strides* di; tsa::Strides* dst; } side[2] = {
+      {"Q", Q, Q_out, d->Hq, &d->q_stride_b, &d->q_out_stride_b, &a.q, &a.qo}, {"K", K, K_out, d->Hkv, &d->k_stride_b, &d->k_out_stride_b, &a.k, &a.ko}};
+  for (auto& t : side) {
+    if (!t.in) continue;
+    if (t.heads < 1 || t.heads > 65535) return fail(TSA_ERR_ARG, "heads of %s (%d) must lie in [1, 65535]", t.name, t.heads);
+    if ((rc = check_ptr(t.in, t.name)) || (rc = check_ptr(t.out, t.name))) return rc;
+    if ((rc = check_layout(t.name, t.si[0], t.si[1], t.si[2], d->B, t.heads, d->L, d->d, t.di)) ||
+        (rc = check_layout(t.name, t.so[0], t.so[1], t.so[2], d->B, t.heads, d->L, d->d, t.dst)))
+      return rc;
+    if (t.in == t.out && (t.di->b != t.dst->b || t.di->h != t.dst->h || t.di->l != t.dst->l))
+      return fail(TSA_ERR_ARG, "%s is its own output under other strides", t.name);
+  }
+  for (int i = 0; i < tsa::kRotaryFreqs; ++i) a.turns[i] = 0;
+  for (int i = 0; i < d->rot / 2; ++i) {
+    if (!std::isfinite(d->freq[i])) return fail(TSA_ERR_ARG, "freq[%d] is not finite", i);
+    // whole turns per position change nothing; what is left, in [0, 1), as a fraction of 2^64
+    const long double turns = (long double)d->freq[i] / 6.283185307179586476925286766559L, part = turns - std::floor(turns);
+    a.turns[i] = part >= 1.0L ? 0 : (uint64_t)std::ldexp(part, 64);
+  }
+  return hip_status(tsa::launch_rotary(a, (hipStream_t)stream), "tsa_rotary");
+}
+
+int tsa_rotary_frequencies(int32_t kind, int32_t rot, double base, double factor, double original, double high, double low,
+                           double* freq, float* gain) {
+  if (!freq || !gain) return fail(TSA_ERR_ARG, "freq or gain is NULL");
+  if (kind < TSA_ROTARY_PLAIN || kind > TSA_ROTARY_WAVELENGTH) return fail(TSA_ERR_ARG, "kind %d is none of TSA_ROTARY_*", kind);
+  if (rot < 2 || rot % 2 != 0 || rot > 2 * TSA_ROTARY_MAX_FREQS) return fail(TSA_ERR_ARG, "rot (%d) must be even and lie in [2, %d]", rot, 2 * TSA_ROTARY_MAX_FREQS);
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(TSA_ERR_ARG, "base must be finite and above 1");
+  const bool by_turns = kind == TSA_ROTARY_PARTS || kind == TSA_ROTARY_WAVELENGTH;
+  if (kind != TSA_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(TSA_ERR_ARG, "factor must be finite and at least 1");
+  if (by_turns) {
+    if (!(original > 0.0) || !std::isfinite(original)) return fail(TSA_ERR_ARG, "original must be finite and positive");
+    if (high == 0.0 && low == 0.0) { high = kind == TSA_ROTARY_PARTS ? 32.0 : 4.0; low = 1.0; }
+    if (!(low > 0.0) || !(high > low) || !std::isfinite(high)) return fail(TSA_ERR_ARG, "0 < low < high (or both 0)");
+  }
+  if (kind == TSA_ROTARY_BASE) {
+    if (rot < 4) return fail(TSA_ERR_ARG, "rot must be at least 4 to raise the base");
+    base *= std::pow(factor, rot / (rot - 2.0));
+  }
+  const double two_pi = 6.283185307179586476925287;
+  double first = 0.0, last = 0.0;
+  if (kind == TSA_ROTARY_PARTS) {
+    // index of the pair with that many turns within the original length
+    const auto at = [&](double turns) { return rot * std::log(original / (turns * two_pi)) / (2.0 * std::log(base)); };
+    first = std::fmax(0.0, std::floor(at(high)));
+    last = std::fmin(rot - 1.0, std::ceil(at(low)));
+  }
+  *gain = kind == TSA_ROTARY_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  for (int32_t i = 0; i < rot / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rot);
+    double stretched = 0.0;                                // share of the pair that is stretched
+    if (kind == TSA_ROTARY_LINEAR) stretched = 1.0;
+    if (kind == TSA_ROTARY_PARTS) stretched = (i - first) / (last > first ? last - first : 0.001);
+    if (kind == TSA_ROTARY_WAVELENGTH) stretched = 1.0 - (original * f / two_pi - low) / (high - low);
+    stretched = std::fmin(1.0, std::fmax(0.0, stretched));
+    freq[i] = kind == TSA_ROTARY_PLAIN || kind == TSA_ROTARY_BASE ? f : f * (1.0 - stretched) + f / factor * stretched;
+  }
+  return TSA_OK;
+}
+
 int tsa_mfma_probe(const void* operands, int32_t iters, int32_t blocks, float* sink, int64_t* clocks,
                    double* flops, int32_t* wall_clock_khz, void* stream) {
   int rc;

@@ -138,4 +138,19 @@ hipError_t launch_read_probe(const void* src, size_t bytes, void* sink, hipStrea
 // probe.hip: streaming copy of `bytes` bytes (a multiple of 16)
 hipError_t launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream_t st);
 
+// rotary.hip: strides as in Dims; turns: turns per position of every pair as a fraction of 2^64
+constexpr int kRotaryFreqs = 64;
+struct RotaryArgs {
+  const void* Q;
+  const void* K;
+  void* Qo;
+  void* Ko;
+  const int32_t* positions;
+  int B, Hq, Hkv, L, d, rot, interleaved, start;
+  float gain;
+  Strides q, k, qo, ko;
+  uint64_t turns[kRotaryFreqs];
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t st);
+
 }  // namespace tsa
