@@ -328,6 +328,50 @@ enum { TSA_ROTARY_PLAIN = 0, TSA_ROTARY_LINEAR = 1, TSA_ROTARY_BASE = 2, TSA_ROT
 int tsa_rotary_frequencies(int32_t kind, int32_t rot, double base, double factor, double original, double high, double low,
                            double* freq, float* gain);
 
+/* ---- The paged cache: K and V of the tokens behind a model's prefill, in pages of a pool that all sequences share.
+ *
+ * k_pages, v_pages: [n_pages, Hkv, page_size, d], device.  TSA_CACHE_BF16: bf16.  TSA_CACHE_E4M3: one byte per element (4 exponent,
+ *   3 mantissa bits, largest finite value 448), with k_scales, v_scales [n_pages, Hkv, page_size] bytes: the row is its elements times
+ *   2^(byte - 127), byte in [1, 254].  (NULL with TSA_CACHE_BF16.)
+ * page_table: int32 [n_seqs, max_pages], device: position p of sequence i is on page page_table[i][p / page_size], row p % page_size.
+ *   An id outside [0, n_pages) is a page that is not there (given back, or never taken): nothing is written to it, its keys are seen by no
+ *   query, it reads back as zeros.  A page that several sequences share must not be written by two of them in one call.
+ * kv_len: int32 [n_seqs], device: tokens of each sequence, the new ones of this step among them (0 .. max_pages * page_size).
+ * cu_q: int32 [n_seqs + 1], device, ascending from 0: the new tokens of sequence i are rows cu_q[i] .. cu_q[i + 1] - 1 of the packed
+ *   tensors Q, K, V, O [n_tokens, heads, d], at the positions kv_len[i] - (cu_q[i + 1] - cu_q[i]) .. kv_len[i] - 1.  Any number of them,
+ *   none included; a token whose position is negative is not written and sees nothing.  Rows from cu_q[n_seqs] on are left as they are.
+ * Lengths, tables and cu_q are read on the device when the work runs: no call waits for them, and a captured graph can be replayed
+ * with others.  Whatever they hold, no access leaves the tensors that the descriptor describes. */
+enum { TSA_CACHE_BF16 = 0, TSA_CACHE_E4M3 = 1 };
+typedef struct tsa_cache_desc {
+  int32_t n_seqs;           /* >= 1 */
+  int32_t n_tokens;         /* rows of the packed tensors, >= 0 (0: nothing to do) */
+  int32_t max_q;            /* most new tokens of a sequence, as far as the caller knows (0: no idea); the result does not depend on it */
+  int32_t Hq, Hkv;          /* Hq % Hkv == 0 */
+  int32_t d;                /* 64 or 128 */
+  int32_t page_size;        /* 16, 32, 64, 128 or 256 */
+  int32_t n_pages;          /* of the pool, >= 1 */
+  int32_t max_pages;        /* of a sequence, >= 1; max_pages * page_size < 2^30 */
+  int32_t format;           /* TSA_CACHE_* */
+  int32_t window;           /* attention: a query at position p sees the keys p - window < t <= p; 0: all t <= p */
+  float scale;              /* attention: softmax scale; 0 means 1/sqrt(d) */
+  /* Element strides of a token and of a head in the packed tensors: both 0 means contiguous; multiples of 8, row (token) strides not 0 */
+  int64_t q_stride_t, q_stride_h;
+  int64_t k_stride_t, k_stride_h;
+  int64_t v_stride_t, v_stride_h;
+  int64_t o_stride_t, o_stride_h;
+} tsa_cache_desc;
+
+/* Writes the new rows of K and V [n_tokens,Hkv,d] bf16 into their pages: as they are, or in 8 bits as e4m3(x 2^-e), nearest even, with
+ * the smallest e >= -126 for which the largest magnitude of the row fits (max |x| <= 448 * 2^e; e = 0 for a row of zeros). */
+int tsa_cache_write(const tsa_cache_desc* desc, const void* K, const void* V, const int32_t* cu_q, const int32_t* kv_len,
+                    const int32_t* page_table, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream);
+
+/* Reads the first L positions of every sequence back: K, V [n_seqs,Hkv,L,d] bf16 out, every element written (zeros from position
+ * kv_len[i] on), exactly the values the cache stands for.  What tsa_score, tsa_forward or tsa_attend can go on with. */
+int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales,
+                   const int32_t* kv_len, const int32_t* page_table, int32_t L, void* K, void* V, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

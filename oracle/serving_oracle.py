@@ -16,3 +16,61 @@ def rotary(x_bits, positions, freq, gain=1.0, interleaved=False):
     out[..., first] = gain * (x[..., first] * np.cos(a) - x[..., second] * np.sin(a))
     out[..., second] = gain * (x[..., first] * np.sin(a) + x[..., second] * np.cos(a))
     return out
+
+
+E4M3_VALUES = np.array([m * 2.0 ** -9 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7) for e in range(16) for m in range(8)][:127])
+
+
+def e4m3_code(x):
+    """Code of the nearest value of the format (of two as near, the one with the even code); |x| <= 448."""
+    x = np.asarray(x, dtype=np.float64)
+    y = np.abs(x)
+    hi = np.clip(np.searchsorted(E4M3_VALUES, y), 1, 126)
+    lo = hi - 1
+    down, up = y - E4M3_VALUES[lo], E4M3_VALUES[hi] - y
+    code = np.where((down < up) | ((down == up) & (lo % 2 == 0)), lo, hi)
+    return (code | np.where(np.signbit(x), 128, 0)).astype(np.uint8)
+
+
+def e4m3_value(code):
+    code = np.asarray(code, dtype=np.int64)
+    return np.where(code & 128, -1.0, 1.0) * E4M3_VALUES[code & 127]
+
+
+def quantise_rows(x_bits):
+    """Rows of bf16 as (codes, bytes): x = e4m3(code) * 2^(byte - 127) up to the rounding of the code."""
+    x = bf16_to_f64(x_bits)
+    big = np.abs(x).max(-1)
+    e = np.full(big.shape, -126, dtype=np.int64)
+    for k in range(-126, 128):                            # the smallest e with big <= 448 * 2^e
+        e = np.where((big > 448.0 * 2.0 ** (k - 1)) & (k > -126), k, e)
+    e = np.where(big == 0, 0, e)
+    return e4m3_code(x / 2.0 ** e[..., None].astype(np.float64)), (e + 127).astype(np.uint8)
+
+
+def places(cu_q, kv_len, table, page_size, n_pages, n_tokens):
+    """(token, page, row of the page) of every new token that is written."""
+    out = []
+    for i in range(len(kv_len)):
+        for t in range(cu_q[i], min(cu_q[i + 1], n_tokens)):
+            p = kv_len[i] - (cu_q[i + 1] - t)
+            if p >= 0 and 0 <= table[i][p // page_size] < n_pages:
+                out.append((t, table[i][p // page_size], p % page_size))
+    return out
+
+
+def attend(q, k, v, scale, window=0):
+    """q [n,d] at the last n positions of k, v [L,d] (float64; a row of k that is NaN is a key that is not there) -> out [n,d], lse [n]."""
+    n, L = len(q), len(k)
+    out, lse = np.zeros((n, v.shape[1])), np.full(n, -np.inf)
+    for r in range(n):
+        p = L - n + r
+        keys = [t for t in range(max(0, p - window + 1) if window else 0, p + 1) if not np.isnan(k[t, 0])]
+        if not keys:
+            continue
+        s = (k[keys] @ q[r]) * scale
+        m = s.max()
+        w = np.exp(s - m)
+        out[r] = (w @ v[keys]) / w.sum()
+        lse[r] = m + np.log(w.sum())
+    return out, lse

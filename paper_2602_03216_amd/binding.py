@@ -19,7 +19,8 @@ EXPORTS = ("tsa_version", "tsa_last_error", "tsa_keep_count", "tsa_workspace_byt
            "tsa_select", "tsa_compress", "tsa_attend_workspace_bytes", "tsa_attend", "tsa_decompress", "tsa_compress_v_tiles", "tsa_attend_fused", "tsa_forward",
            "tsa_forward_dynamic_workspace_bytes", "tsa_forward_dynamic",
            "tsa_layer_drift_workspace_bytes", "tsa_layer_drift", "tsa_sparse_layers", "tsa_mfma_probe", "tsa_mix_probe", "tsa_read_probe", "tsa_copy_probe", "tsa_bench_set_attend_form",
-           "tsa_select_static", "tsa_select_static_capacity", "tsa_rotary", "tsa_rotary_frequencies")
+           "tsa_select_static", "tsa_select_static_capacity", "tsa_rotary", "tsa_rotary_frequencies",
+           "tsa_cache_write", "tsa_cache_read")
 
 TSA_ROTARY_MAX_FREQS = 64
 TSA_ROTARY_PLAIN, TSA_ROTARY_LINEAR, TSA_ROTARY_BASE, TSA_ROTARY_PARTS, TSA_ROTARY_WAVELENGTH = 0, 1, 2, 3, 4
@@ -66,6 +67,22 @@ def make_rotary_desc(B, Hq, Hkv, L, d, freq, interleaved=0, start=0, gain=1.0, q
         raise TsaError(TSA_ERR_ARG, "at most %d frequencies" % TSA_ROTARY_MAX_FREQS)
     return tsa_rotary_desc(B, Hq, Hkv, L, d, 2 * len(freq), interleaved, start, gain, 0, *q_strides, *k_strides, *q_out_strides,
                            *k_out_strides, (ctypes.c_double * TSA_ROTARY_MAX_FREQS)(*[float(f) for f in freq]))
+
+
+TSA_CACHE_BF16, TSA_CACHE_E4M3 = 0, 1
+
+
+class tsa_cache_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "max_q", "Hq", "Hkv", "d", "page_size", "n_pages", "max_pages", "format",
+                                              "window")] + [("scale", ctypes.c_float)] + \
+               [("%s_stride_%s" % (t, a), ctypes.c_int64) for t in "qkvo" for a in "th"]
+
+
+def make_cache_desc(n_seqs, n_tokens, Hq, Hkv, d, page_size, n_pages, max_pages, format=TSA_CACHE_BF16, max_q=0, window=0, scale=0.0,
+                    q_strides=(0, 0), k_strides=(0, 0), v_strides=(0, 0), o_strides=(0, 0)):
+    """*_strides = (stride of a token, stride of a head) in elements of the packed tensors; zeros = contiguous [n_tokens, heads, d]."""
+    return tsa_cache_desc(n_seqs, n_tokens, max_q, Hq, Hkv, d, page_size, n_pages, max_pages, format, window, scale,
+                          *q_strides, *k_strides, *v_strides, *o_strides)
 
 
 _lib = None
@@ -152,6 +169,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     dbl = ctypes.c_double
     lib.tsa_rotary_frequencies.restype = ctypes.c_int
     lib.tsa_rotary_frequencies.argtypes = [i32, i32, dbl, dbl, dbl, dbl, dbl, ctypes.POINTER(dbl), ctypes.POINTER(ctypes.c_float)]
+    cp = ctypes.POINTER(tsa_cache_desc)
+    lib.tsa_cache_write.restype = ctypes.c_int
+    lib.tsa_cache_write.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.tsa_cache_read.restype = ctypes.c_int
+    lib.tsa_cache_read.argtypes = [cp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -356,6 +378,41 @@ def tsa_rotary(desc, Q, K, Q_out, K_out, positions=None):
     _check(load_library().tsa_rotary(ctypes.byref(desc), at(Q, desc.Hq, "q", "Q"), at(K, desc.Hkv, "k", "K"),
                                      _view(positions, torch.int32, (desc.B, desc.L), "positions"),
                                      at(Q_out, desc.Hq, "q_out", "Q_out"), at(K_out, desc.Hkv, "k_out", "K_out"), _stream()))
+
+
+_POOL_TYPES = {TSA_CACHE_BF16: (torch.bfloat16,), TSA_CACHE_E4M3: (torch.uint8, torch.float8_e4m3fn)}
+
+
+def _cache(desc, k_pages, v_pages, k_scales, v_scales):
+    shape = (desc.n_pages, desc.Hkv, desc.page_size, desc.d)
+    kind = _POOL_TYPES.get(desc.format, ())
+    return (_view(k_pages, kind, shape, "k_pages"), _view(v_pages, kind, shape, "v_pages"),
+            _view(k_scales, torch.uint8, shape[:3], "k_scales"), _view(v_scales, torch.uint8, shape[:3], "v_scales"))
+
+
+def _lengths(desc, kv_len, page_table):
+    return _view(kv_len, torch.int32, (desc.n_seqs,), "kv_len"), _view(page_table, torch.int32, (desc.n_seqs, desc.max_pages), "page_table")
+
+
+def _packed(desc, t, heads, which, name):
+    return _view(t, torch.bfloat16, (desc.n_tokens, heads, desc.d), name,
+                 (getattr(desc, "%s_stride_t" % which), getattr(desc, "%s_stride_h" % which)))
+
+
+def tsa_cache_write(desc, K, V, cu_q, kv_len, page_table, k_pages, v_pages, k_scales=None, v_scales=None):
+    """K, V [n_tokens,Hkv,d] bf16 (views with the descriptor's strides); pools bf16, or uint8 / float8_e4m3fn with uint8 scales."""
+    kp, vp_, ks, vs = _cache(desc, k_pages, v_pages, k_scales, v_scales)
+    _check(load_library().tsa_cache_write(ctypes.byref(desc), _packed(desc, K, desc.Hkv, "k", "K"), _packed(desc, V, desc.Hkv, "v", "V"),
+                                          _view(cu_q, torch.int32, (desc.n_seqs + 1,), "cu_q"), *_lengths(desc, kv_len, page_table),
+                                          kp, vp_, ks, vs, _stream()))
+
+
+def tsa_cache_read(desc, k_pages, v_pages, kv_len, page_table, L, K, V, k_scales=None, v_scales=None):
+    """K, V [n_seqs,Hkv,L,d] bf16, contiguous: the first L positions of every sequence."""
+    shape = (desc.n_seqs, desc.Hkv, L, desc.d)
+    _check(load_library().tsa_cache_read(ctypes.byref(desc), *_cache(desc, k_pages, v_pages, k_scales, v_scales),
+                                         *_lengths(desc, kv_len, page_table), L, _view(K, torch.bfloat16, shape, "K"),
+                                         _view(V, torch.bfloat16, shape, "V"), _stream()))
 
 
 def tsa_mfma_probe(operands, iters, blocks, sink, clocks):

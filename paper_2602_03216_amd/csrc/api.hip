@@ -608,6 +608,98 @@ int tsa_rotary_frequencies(int32_t kind, int32_t rot, double base, double factor
   return TSA_OK;
 }
 
+namespace {
+
+// Layout of a packed [n_tokens,heads,d] tensor (both strides 0: contiguous).
+int check_packed(const char* name, int64_t t, int64_t h, int heads, int d, long long* t_out, long long* h_out) {
+  if (t == 0 && h == 0) {
+    *t_out = (long long)heads * d;
+    *h_out = d;
+    return TSA_OK;
+  }
+  if (t < d || h < 0 || (t | h) % 8 != 0) return fail(TSA_ERR_ARG, "%s strides: multiples of 8 elements, stride_t >= d, none negative (or both 0)", name);
+  if (heads > 1 && h < d && h != 0) return fail(TSA_ERR_ARG, "%s_stride_h is below d", name);
+  if (heads > 1 && h == 0) return fail(TSA_ERR_ARG, "%s_stride_h is 0", name);
+  if (t > ((int64_t)1 << 30) || h > ((int64_t)1 << 46)) return fail(TSA_ERR_UNSUPPORTED, "%s strides too large", name);
+  *t_out = t;
+  *h_out = h;
+  return TSA_OK;
+}
+
+int check_cache_desc(const tsa_cache_desc* d, tsa::CacheArgs* c) {
+  int rc;
+  if (!d) return fail(TSA_ERR_ARG, "desc is NULL");
+  if (d->n_seqs < 1 || d->n_tokens < 0 || d->max_q < 0) return fail(TSA_ERR_ARG, "n_seqs must be >= 1, n_tokens and max_q >= 0");
+  if (d->n_seqs > (1 << 20) || d->n_tokens > (1 << 26)) return fail(TSA_ERR_UNSUPPORTED, "at most 2^20 sequences and 2^26 new tokens");
+  if (d->Hq < 1 || d->Hkv < 1 || d->Hq % d->Hkv != 0) return fail(TSA_ERR_ARG, "Hq (%d) is not a multiple of Hkv (%d)", d->Hq, d->Hkv);
+  if (d->Hq > 1024) return fail(TSA_ERR_UNSUPPORTED, "Hq (%d): at most 1024", d->Hq);
+  if (d->d != 64 && d->d != 128) return fail(TSA_ERR_UNSUPPORTED, "head dimension %d: only 64 and 128 are built", d->d);
+  if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)) != 0)
+    return fail(TSA_ERR_UNSUPPORTED, "page_size %d: 16, 32, 64, 128 and 256 are built", d->page_size);
+  if (d->n_pages < 1 || d->max_pages < 1) return fail(TSA_ERR_ARG, "n_pages and max_pages must be >= 1");
+  if ((long long)d->max_pages * d->page_size >= (1LL << 30)) return fail(TSA_ERR_UNSUPPORTED, "max_pages * page_size must stay below 2^30");
+  if (d->format != TSA_CACHE_BF16 && d->format != TSA_CACHE_E4M3) return fail(TSA_ERR_ARG, "format %d is none of TSA_CACHE_*", d->format);
+  if (d->window < 0) return fail(TSA_ERR_ARG, "window must be >= 0");
+  if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return fail(TSA_ERR_ARG, "scale must be finite and >= 0");
+  c->n_seqs = d->n_seqs; c->n_tokens = d->n_tokens; c->max_q = d->max_q; c->Hq = d->Hq; c->Hkv = d->Hkv; c->d = d->d;
+  c->page_log2 = __builtin_ctz((unsigned)d->page_size);
+  c->n_pages = d->n_pages; c->max_pages = d->max_pages; c->e4m3 = d->format == TSA_CACHE_E4M3; c->window = d->window;
+  c->scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)d->d);
+  if ((rc = check_packed("q", d->q_stride_t, d->q_stride_h, d->Hq, d->d, &c->q_t, &c->q_h)) ||
+      (rc = check_packed("k", d->k_stride_t, d->k_stride_h, d->Hkv, d->d, &c->k_t, &c->k_h)) ||
+      (rc = check_packed("v", d->v_stride_t, d->v_stride_h, d->Hkv, d->d, &c->v_t, &c->v_h)) ||
+      (rc = check_packed("o", d->o_stride_t, d->o_stride_h, d->Hq, d->d, &c->o_t, &c->o_h)))
+    return rc;
+  c->cu_q = c->kv_len = c->table = nullptr;
+  c->kp = c->vp = c->ks = c->vs = nullptr;
+  return TSA_OK;
+}
+
+int check_ints(const int32_t* p, const char* name) {
+  if (!p || ((uintptr_t)p & 3u) != 0) return fail(TSA_ERR_ARG, "%s is NULL or not 4-byte aligned", name);
+  return TSA_OK;
+}
+
+// The device side of a cache; writable only as far as the entry point says so itself.
+int check_cache(tsa::CacheArgs* c, const void* k_pages, const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales,
+                const int32_t* kv_len, const int32_t* page_table) {
+  int rc;
+  if ((rc = check_ptr(k_pages, "k_pages")) || (rc = check_ptr(v_pages, "v_pages"))) return rc;
+  if (c->e4m3 && ((rc = check_ptr(k_scales, "k_scales")) || (rc = check_ptr(v_scales, "v_scales")))) return rc;
+  if (!c->e4m3 && (k_scales || v_scales)) return fail(TSA_ERR_ARG, "a bf16 cache has no scales");
+  if ((rc = check_ints(kv_len, "kv_len")) || (rc = check_ints(page_table, "page_table"))) return rc;
+  c->kp = (void*)k_pages; c->vp = (void*)v_pages; c->ks = (void*)k_scales; c->vs = (void*)v_scales;
+  c->kv_len = kv_len; c->table = page_table;
+  return TSA_OK;
+}
+
+}  // namespace
+
+int tsa_cache_write(const tsa_cache_desc* desc, const void* K, const void* V, const int32_t* cu_q, const int32_t* kv_len,
+                    const int32_t* page_table, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream) {
+  tsa::CacheArgs c;
+  int rc;
+  if ((rc = check_cache_desc(desc, &c))) return rc;
+  if (c.n_tokens == 0) return TSA_OK;
+  if ((rc = check_ptr(K, "K")) || (rc = check_ptr(V, "V")) || (rc = check_ints(cu_q, "cu_q"))) return rc;
+  if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
+  c.cu_q = cu_q;
+  return hip_status(tsa::launch_cache_write(c, K, V, (hipStream_t)stream), "tsa_cache_write");
+}
+
+int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales,
+                   const int32_t* kv_len, const int32_t* page_table, int32_t L, void* K, void* V, void* stream) {
+  tsa::CacheArgs c;
+  int rc;
+  if ((rc = check_cache_desc(desc, &c))) return rc;
+  if (L < 0 || L >= (1 << 30)) return fail(TSA_ERR_ARG, "L (%d) must lie in [0, 2^30)", L);
+  if ((long long)c.n_seqs * c.Hkv * ((L + 127LL) / 128) > 0x7fffffffLL) return fail(TSA_ERR_UNSUPPORTED, "grid too large");
+  if (L == 0) return TSA_OK;
+  if ((rc = check_ptr(K, "K")) || (rc = check_ptr(V, "V"))) return rc;
+  if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
+  return hip_status(tsa::launch_cache_read(c, L, K, V, (hipStream_t)stream), "tsa_cache_read");
+}
+
 int tsa_mfma_probe(const void* operands, int32_t iters, int32_t blocks, float* sink, int64_t* clocks,
                    double* flops, int32_t* wall_clock_khz, void* stream) {
   int rc;

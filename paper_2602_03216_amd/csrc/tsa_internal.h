@@ -153,4 +153,20 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t st);
 
+// The paged cache (cache.hip, attend_cache.hip): the descriptor as the launchers take it, strides in elements.
+struct CacheArgs {
+  int n_seqs, n_tokens, max_q, Hq, Hkv, d, page_log2, n_pages, max_pages, e4m3, window;
+  float scale;
+  long long q_t, q_h, k_t, k_h, v_t, v_h, o_t, o_h;
+  const int32_t* cu_q;
+  const int32_t* kv_len;
+  const int32_t* table;
+  void* kp;
+  void* vp;
+  void* ks;
+  void* vs;
+};
+hipError_t launch_cache_write(const CacheArgs& c, const void* K, const void* V, hipStream_t st);
+hipError_t launch_cache_read(const CacheArgs& c, int L, void* K, void* V, hipStream_t st);
+
 }  // namespace tsa
