@@ -345,23 +345,35 @@ def tsa_sparse_layers(drift, delta=0.5):
     return list(out)
 
 
-def _view(t, dtype, shape, name, strides=None):
-    """Address of a tensor that has to be of this type and shape.  strides: element strides of all axes but the last, as the descriptor
-    has them (zeros: contiguous); the tensor's own have to be the same."""
+def _queue():
+    """(handle of the current stream, current device)"""
+    try:
+        st = torch.cuda.current_stream()
+    except (RuntimeError, AssertionError) as e:             # no GPU
+        raise TsaError(TSA_ERR_HIP, str(e)) from None
+    return st.cuda_stream, st.device_index
+
+
+_BF16, _I32, _U8, _F32 = (torch.bfloat16,), (torch.int32,), (torch.uint8,), (torch.float32,)
+
+
+def _view(t, dev, dtypes, shape, name, strides=None):
+    """Address of a tensor that has to be on device `dev`, of one of these types and of this shape.  strides: element strides of all axes
+    but the last, as the descriptor has them (None or zeros: contiguous); the tensor's own have to be the same."""
     if t is None:
         return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise TsaError(TSA_ERR_ARG, "%s is not on the current GPU" % name)
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    if t.dtype not in dtypes:
         raise TsaError(TSA_ERR_ARG, "%s is %s" % (name, t.dtype))
-    if tuple(t.shape) != tuple(shape):
-        raise TsaError(TSA_ERR_ARG, "%s is %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.shape != shape:
+        raise TsaError(TSA_ERR_ARG, "%s is %s, not %s" % (name, tuple(t.shape), shape))
     if strides is None or not any(strides):
         if not t.is_contiguous():
             raise TsaError(TSA_ERR_ARG, "%s is not contiguous" % name)
-    elif any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), (*strides, 1))):
+    elif t.stride() != (*strides, 1) and any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), (*strides, 1))):
         raise TsaError(TSA_ERR_ARG, "%s has strides %s, the descriptor %s" % (name, t.stride(), tuple(strides)))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def tsa_rotary_frequencies(kind, rot, base, factor=1.0, original=0.0, high=0.0, low=0.0):
@@ -373,46 +385,48 @@ def tsa_rotary_frequencies(kind, rot, base, factor=1.0, original=0.0, high=0.0, 
 
 def tsa_rotary(desc, Q, K, Q_out, K_out, positions=None):
     """Q [B,Hq,L,d], K [B,Hkv,L,d] and their outputs: bf16 tensors or views with the descriptor's strides; positions int32 [B,L]."""
-    def at(t, heads, which, name):
-        return _view(t, torch.bfloat16, (desc.B, heads, desc.L, desc.d), name, [getattr(desc, "%s_stride_%s" % (which, x)) for x in "bhl"])
-    _check(load_library().tsa_rotary(ctypes.byref(desc), at(Q, desc.Hq, "q", "Q"), at(K, desc.Hkv, "k", "K"),
-                                     _view(positions, torch.int32, (desc.B, desc.L), "positions"),
-                                     at(Q_out, desc.Hq, "q_out", "Q_out"), at(K_out, desc.Hkv, "k_out", "K_out"), _stream()))
+    st, dev = _queue()
+    B, L, d = desc.B, desc.L, desc.d
+    q, k = (B, desc.Hq, L, d), (B, desc.Hkv, L, d)
+    _check(load_library().tsa_rotary(
+        ctypes.byref(desc), _view(Q, dev, _BF16, q, "Q", (desc.q_stride_b, desc.q_stride_h, desc.q_stride_l)),
+        _view(K, dev, _BF16, k, "K", (desc.k_stride_b, desc.k_stride_h, desc.k_stride_l)), _view(positions, dev, _I32, (B, L), "positions"),
+        _view(Q_out, dev, _BF16, q, "Q_out", (desc.q_out_stride_b, desc.q_out_stride_h, desc.q_out_stride_l)),
+        _view(K_out, dev, _BF16, k, "K_out", (desc.k_out_stride_b, desc.k_out_stride_h, desc.k_out_stride_l)), st))
 
 
 _POOL_TYPES = {TSA_CACHE_BF16: (torch.bfloat16,), TSA_CACHE_E4M3: (torch.uint8, torch.float8_e4m3fn)}
 
 
-def _cache(desc, k_pages, v_pages, k_scales, v_scales):
+def _cache(desc, dev, k_pages, v_pages, k_scales, v_scales):
     shape = (desc.n_pages, desc.Hkv, desc.page_size, desc.d)
     kind = _POOL_TYPES.get(desc.format, ())
-    return (_view(k_pages, kind, shape, "k_pages"), _view(v_pages, kind, shape, "v_pages"),
-            _view(k_scales, torch.uint8, shape[:3], "k_scales"), _view(v_scales, torch.uint8, shape[:3], "v_scales"))
+    return (_view(k_pages, dev, kind, shape, "k_pages"), _view(v_pages, dev, kind, shape, "v_pages"),
+            _view(k_scales, dev, _U8, shape[:3], "k_scales"), _view(v_scales, dev, _U8, shape[:3], "v_scales"))
 
 
-def _lengths(desc, kv_len, page_table):
-    return _view(kv_len, torch.int32, (desc.n_seqs,), "kv_len"), _view(page_table, torch.int32, (desc.n_seqs, desc.max_pages), "page_table")
-
-
-def _packed(desc, t, heads, which, name):
-    return _view(t, torch.bfloat16, (desc.n_tokens, heads, desc.d), name,
-                 (getattr(desc, "%s_stride_t" % which), getattr(desc, "%s_stride_h" % which)))
+def _lengths(desc, dev, kv_len, page_table):
+    n = desc.n_seqs
+    return _view(kv_len, dev, _I32, (n,), "kv_len"), _view(page_table, dev, _I32, (n, desc.max_pages), "page_table")
 
 
 def tsa_cache_write(desc, K, V, cu_q, kv_len, page_table, k_pages, v_pages, k_scales=None, v_scales=None):
     """K, V [n_tokens,Hkv,d] bf16 (views with the descriptor's strides); pools bf16, or uint8 / float8_e4m3fn with uint8 scales."""
-    kp, vp_, ks, vs = _cache(desc, k_pages, v_pages, k_scales, v_scales)
-    _check(load_library().tsa_cache_write(ctypes.byref(desc), _packed(desc, K, desc.Hkv, "k", "K"), _packed(desc, V, desc.Hkv, "v", "V"),
-                                          _view(cu_q, torch.int32, (desc.n_seqs + 1,), "cu_q"), *_lengths(desc, kv_len, page_table),
-                                          kp, vp_, ks, vs, _stream()))
+    st, dev = _queue()
+    rows = (desc.n_tokens, desc.Hkv, desc.d)
+    _check(load_library().tsa_cache_write(
+        ctypes.byref(desc), _view(K, dev, _BF16, rows, "K", (desc.k_stride_t, desc.k_stride_h)),
+        _view(V, dev, _BF16, rows, "V", (desc.v_stride_t, desc.v_stride_h)), _view(cu_q, dev, _I32, (desc.n_seqs + 1,), "cu_q"),
+        *_lengths(desc, dev, kv_len, page_table), *_cache(desc, dev, k_pages, v_pages, k_scales, v_scales), st))
 
 
 def tsa_cache_read(desc, k_pages, v_pages, kv_len, page_table, L, K, V, k_scales=None, v_scales=None):
     """K, V [n_seqs,Hkv,L,d] bf16, contiguous: the first L positions of every sequence."""
+    st, dev = _queue()
     shape = (desc.n_seqs, desc.Hkv, L, desc.d)
-    _check(load_library().tsa_cache_read(ctypes.byref(desc), *_cache(desc, k_pages, v_pages, k_scales, v_scales),
-                                         *_lengths(desc, kv_len, page_table), L, _view(K, torch.bfloat16, shape, "K"),
-                                         _view(V, torch.bfloat16, shape, "V"), _stream()))
+    _check(load_library().tsa_cache_read(ctypes.byref(desc), *_cache(desc, dev, k_pages, v_pages, k_scales, v_scales),
+                                         *_lengths(desc, dev, kv_len, page_table), L, _view(K, dev, _BF16, shape, "K"),
+                                         _view(V, dev, _BF16, shape, "V"), st))
 
 
 def tsa_mfma_probe(operands, iters, blocks, sink, clocks):
