@@ -372,6 +372,18 @@ int tsa_cache_write(const tsa_cache_desc* desc, const void* K, const void* V, co
 int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales,
                    const int32_t* kv_len, const int32_t* page_table, int32_t L, void* K, void* V, void* stream);
 
+/* Attention of the new tokens over the cache, which holds them already (tsa_cache_write first): token t of sequence i at position
+ * p = kv_len[i] - (cu_q[i + 1] - t) sees the keys at positions <= p of its sequence (within the window, if the descriptor has one) that are
+ * on pages that are there.  Single tokens, drafted tokens, pieces of prompts and whole prompts, mixed as they come.
+ *   Q [n_tokens,Hq,d] bf16;  O [n_tokens,Hq,d] bf16 out;  lse [n_tokens,Hq] fp32 out or NULL (natural-log sum-exp of the scaled logits)
+ *   A token that sees no key gets zeros and -infinity.
+ *   ws: tsa_attend_cache_workspace_bytes(desc) bytes; its contents need not be kept between calls
+ * Arithmetic as in tsa_attend; 8-bit rows are widened exactly. The same inputs give the same bits. */
+size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc);
+int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                     const uint8_t* v_scales, const int32_t* cu_q, const int32_t* kv_len, const int32_t* page_table,
+                     void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -59,18 +59,19 @@ def places(cu_q, kv_len, table, page_size, n_pages, n_tokens):
     return out
 
 
-def attend(q, k, v, scale, window=0):
-    """q [n,d] at the last n positions of k, v [L,d] (float64; a row of k that is NaN is a key that is not there) -> out [n,d], lse [n]."""
+def attend(q, k, v, there, scale, window=0):
+    """q [n,d] at the last n positions of k, v [L,d] (float64); there [L]: whether a key's page is -> out [n,d], lse [n], and the same
+    average of |v| (what an error of the probabilities is measured by)."""
     n, L = len(q), len(k)
-    out, lse = np.zeros((n, v.shape[1])), np.full(n, -np.inf)
-    for r in range(n):
-        p = L - n + r
-        keys = [t for t in range(max(0, p - window + 1) if window else 0, p + 1) if not np.isnan(k[t, 0])]
-        if not keys:
-            continue
-        s = (k[keys] @ q[r]) * scale
-        m = s.max()
-        w = np.exp(s - m)
-        out[r] = (w @ v[keys]) / w.sum()
-        lse[r] = m + np.log(w.sum())
-    return out, lse
+    p, t = np.arange(L - n, L)[:, None], np.arange(L)[None, :]
+    seen = (t <= p) & there[None, :]
+    if window:
+        seen &= t > p - window
+    s = np.where(seen, (q @ np.where(there[:, None], k, 0.0).T) * scale, -np.inf)
+    m = s.max(-1, keepdims=True, initial=-1e300)
+    w = np.exp(s - m)
+    l = w.sum(-1, keepdims=True)
+    v = np.where(there[:, None], v, 0.0)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        mean = lambda x: np.where(l > 0, (w @ x) / l, 0.0)
+        return mean(v), np.where(l > 0, m + np.log(l), -np.inf)[:, 0], mean(np.abs(v))

@@ -20,7 +20,7 @@ EXPORTS = ("tsa_version", "tsa_last_error", "tsa_keep_count", "tsa_workspace_byt
            "tsa_forward_dynamic_workspace_bytes", "tsa_forward_dynamic",
            "tsa_layer_drift_workspace_bytes", "tsa_layer_drift", "tsa_sparse_layers", "tsa_mfma_probe", "tsa_mix_probe", "tsa_read_probe", "tsa_copy_probe", "tsa_bench_set_attend_form",
            "tsa_select_static", "tsa_select_static_capacity", "tsa_rotary", "tsa_rotary_frequencies",
-           "tsa_cache_write", "tsa_cache_read")
+           "tsa_cache_write", "tsa_cache_read", "tsa_attend_cache_workspace_bytes", "tsa_attend_cache")
 
 TSA_ROTARY_MAX_FREQS = 64
 TSA_ROTARY_PLAIN, TSA_ROTARY_LINEAR, TSA_ROTARY_BASE, TSA_ROTARY_PARTS, TSA_ROTARY_WAVELENGTH = 0, 1, 2, 3, 4
@@ -174,6 +174,10 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.tsa_cache_write.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.tsa_cache_read.restype = ctypes.c_int
     lib.tsa_cache_read.argtypes = [cp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.tsa_attend_cache_workspace_bytes.restype = sz
+    lib.tsa_attend_cache_workspace_bytes.argtypes = [cp]
+    lib.tsa_attend_cache.restype = ctypes.c_int
+    lib.tsa_attend_cache.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -427,6 +431,25 @@ def tsa_cache_read(desc, k_pages, v_pages, kv_len, page_table, L, K, V, k_scales
     _check(load_library().tsa_cache_read(ctypes.byref(desc), *_cache(desc, dev, k_pages, v_pages, k_scales, v_scales),
                                          *_lengths(desc, dev, kv_len, page_table), L, _view(K, dev, _BF16, shape, "K"),
                                          _view(V, dev, _BF16, shape, "V"), st))
+
+
+def alloc_attend_cache_workspace(desc, device="cuda"):
+    """Device buffer of tsa_attend_cache_workspace_bytes() bytes."""
+    n = load_library().tsa_attend_cache_workspace_bytes(ctypes.byref(desc))
+    if n == 0:
+        raise TsaError(TSA_ERR_ARG, tsa_last_error())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def tsa_attend_cache(desc, Q, k_pages, v_pages, cu_q, kv_len, page_table, O, ws, lse=None, k_scales=None, v_scales=None):
+    """Q, O [n_tokens,Hq,d] bf16 (views with the descriptor's strides), lse [n_tokens,Hq] fp32 or None; pools as in tsa_cache_write."""
+    st, dev = _queue()
+    rows = (desc.n_tokens, desc.Hq, desc.d)
+    _check(load_library().tsa_attend_cache(
+        ctypes.byref(desc), _view(Q, dev, _BF16, rows, "Q", (desc.q_stride_t, desc.q_stride_h)), *_cache(desc, dev, k_pages, v_pages, k_scales, v_scales),
+        _view(cu_q, dev, _I32, (desc.n_seqs + 1,), "cu_q"), *_lengths(desc, dev, kv_len, page_table),
+        _view(O, dev, _BF16, rows, "O", (desc.o_stride_t, desc.o_stride_h)), _view(lse, dev, _F32, rows[:2], "lse"),
+        _view(ws, dev, _U8, ws.shape, "ws"), ws.numel(), st))
 
 
 def tsa_mfma_probe(operands, iters, blocks, sink, clocks):

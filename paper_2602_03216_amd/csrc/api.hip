@@ -632,6 +632,7 @@ int check_cache_desc(const tsa_cache_desc* d, tsa::CacheArgs* c) {
   if (d->n_seqs < 1 || d->n_tokens < 0 || d->max_q < 0) return fail(TSA_ERR_ARG, "n_seqs must be >= 1, n_tokens and max_q >= 0");
   if (d->n_seqs > (1 << 20) || d->n_tokens > (1 << 26)) return fail(TSA_ERR_UNSUPPORTED, "at most 2^20 sequences and 2^26 new tokens");
   if (d->Hq < 1 || d->Hkv < 1 || d->Hq % d->Hkv != 0) return fail(TSA_ERR_ARG, "Hq (%d) is not a multiple of Hkv (%d)", d->Hq, d->Hkv);
+  if ((long long)d->n_tokens * (d->Hq / d->Hkv) > (1 << 30)) return fail(TSA_ERR_UNSUPPORTED, "n_tokens * Hq / Hkv above 2^30");
   if (d->Hq > 1024) return fail(TSA_ERR_UNSUPPORTED, "Hq (%d): at most 1024", d->Hq);
   if (d->d != 64 && d->d != 128) return fail(TSA_ERR_UNSUPPORTED, "head dimension %d: only 64 and 128 are built", d->d);
   if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)) != 0)
@@ -643,7 +644,7 @@ int check_cache_desc(const tsa_cache_desc* d, tsa::CacheArgs* c) {
   if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return fail(TSA_ERR_ARG, "scale must be finite and >= 0");
   c->n_seqs = d->n_seqs; c->n_tokens = d->n_tokens; c->max_q = d->max_q; c->Hq = d->Hq; c->Hkv = d->Hkv; c->d = d->d;
   c->page_log2 = __builtin_ctz((unsigned)d->page_size);
-  c->n_pages = d->n_pages; c->max_pages = d->max_pages; c->e4m3 = d->format == TSA_CACHE_E4M3; c->window = d->window;
+  c->n_pages = d->n_pages; c->max_pages = d->max_pages; c->e4m3 = d->format == TSA_CACHE_E4M3; c->window = d->window < (1 << 30) ? d->window : 0;      // (as long as any sequence: none)
   c->scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)d->d);
   if ((rc = check_packed("q", d->q_stride_t, d->q_stride_h, d->Hq, d->d, &c->q_t, &c->q_h)) ||
       (rc = check_packed("k", d->k_stride_t, d->k_stride_h, d->Hkv, d->d, &c->k_t, &c->k_h)) ||
@@ -698,6 +699,27 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
   if ((rc = check_ptr(K, "K")) || (rc = check_ptr(V, "V"))) return rc;
   if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
   return hip_status(tsa::launch_cache_read(c, L, K, V, (hipStream_t)stream), "tsa_cache_read");
+}
+
+size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc) {
+  tsa::CacheArgs c;
+  if (check_cache_desc(desc, &c) != TSA_OK) return 0;
+  return tsa::attend_cache_ws_bytes(c);
+}
+
+int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                     const uint8_t* v_scales, const int32_t* cu_q, const int32_t* kv_len, const int32_t* page_table,
+                     void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  tsa::CacheArgs c;
+  int rc;
+  if ((rc = check_cache_desc(desc, &c))) return rc;
+  if (c.n_tokens == 0) return TSA_OK;
+  if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(O, "O")) || (rc = check_ints(cu_q, "cu_q"))) return rc;
+  if (lse && ((uintptr_t)lse & 3u)) return fail(TSA_ERR_ARG, "lse is not 4-byte aligned");
+  if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
+  if ((rc = check_ws(ws, ws_bytes, tsa::attend_cache_ws_bytes(c)))) return rc;
+  c.cu_q = cu_q;
+  return hip_status(tsa::launch_attend_cache(c, Q, O, lse, ws, (hipStream_t)stream), "tsa_attend_cache");
 }
 
 int tsa_mfma_probe(const void* operands, int32_t iters, int32_t blocks, float* sink, int64_t* clocks,

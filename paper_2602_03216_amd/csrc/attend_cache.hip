@@ -1,0 +1,507 @@
+// Attention of the new tokens of a ragged batch over the paged cache:
+//   o_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j of t's sequence with p_t - window < j <= p_t.
+//
+// The g query heads of a KV head and the new tokens of a sequence are the rows of one matrix: row r is token r / g, head r % g of
+// the group, so K and V are read once for all of them.
+//
+// Few rows per sequence (single tokens, drafted tokens): K and V are what has to be read, HBM bounds it, and the keys are the axis that
+// fills the chip.  The work of the whole batch, counted in steps of 128 keys of one (sequence, KV head, tile of 16 rows), is cut into
+// equal shares, one per workgroup; lengths are known on the device only, so every workgroup sums them up itself and finds its
+// place.  A share that covers only a part of a row tile's keys leaves its running max, sum and output in the workspace, and a second launch
+// joins them; whole ones are written at once.
+//   A wavefront takes 32 keys of a step, with a softmax of its own; the four meet at the end of a segment.  S^T = K Q^T on
+// v_mfma_f32_16x16x32_bf16: rows = keys, columns = the tile's rows, so a lane keeps one row's max and sum.  K goes from memory straight
+// into the registers of that product (a lane's 16 bytes are its operand).  O^T = V^T P^T takes the probabilities as the lane holds them: its
+// contraction index runs over keys 4 q .. 4 q + 3 of the first 16 and of the second 16 keys (q = lane / 16), and V^T comes out of LDS
+// by the transposing reads, four (eight in 8 bits) keys of one column per lane.  V goes to LDS without passing registers; the
+// next step's K and V are in flight while a step is computed, and no wavefront waits for another inside a segment.
+//   8 bits: K is widened to bf16 with its row's power of two by the conversion (exact), V without it, and V's power goes into the
+// probability in front of its rounding.
+#include "cache_common.h"
+
+namespace tsa {
+
+using namespace cache_detail;
+
+namespace {
+
+constexpr float kNone = -1.0e30f;                        // running max of a row that has seen no key
+constexpr float kLag = 8.0f;                             // log2 units that the running max may lag behind
+constexpr int kStep = 128;                               // keys of a step
+constexpr int kShares = 512;                             // workgroups: two per CU
+
+struct Args {
+  Batch b;
+  const __bf16* Q;
+  const char* kp;
+  const char* vp;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  __bf16* O;
+  float* lse;
+  long long q_t, q_h, o_t, o_h;
+  int Hq, g, window;
+  float c;                       // scale * log2(e)
+  FastDiv by_g;
+  // workspace
+  unsigned long long* before;    // [n_seqs + 1] steps in front of every sequence
+  float* part_o;                 // [2 kShares][RT][d]
+  float* part_ml;                // [2 kShares][RT][2]
+};
+
+__device__ const u32x4 g_zeros[16] = {};                 // a row of V for keys that nobody sees
+
+// 64 lanes' 16 bytes to LDS bytes lds .. lds + 1023.  Counted by vmcnt and by nothing that the compiler tracks; no output register.  The wait
+// states: m0 may come out of a vector instruction.
+__device__ __forceinline__ void load_row_to_lds(const void* p, int lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
+#endif
+}
+// Everything that this wavefront asked for has landed, in registers and in LDS, and its LDS reads are done.
+__device__ __forceinline__ void wait_all() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
+  u32x4 w;
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// What a sequence asks for.
+struct Seq {
+  int q0, q_len, kv, rows, tiles, first, steps;          // first: its first key that any query sees, rounded down to 16
+  __device__ __forceinline__ unsigned long long units(int Hkv) const { return (unsigned long long)Hkv * tiles * steps; }
+};
+
+template <int RT>
+__device__ __forceinline__ Seq sequence(const Args& a, int i) {
+  Seq s;
+  s.q0 = a.b.first(i);
+  s.q_len = max(a.b.first(i + 1) - s.q0, 0);
+  s.kv = a.b.kv(i);
+  s.rows = s.q_len * a.g;
+  s.tiles = (s.rows + RT - 1) / RT;
+  s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
+  s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
+  return s;
+}
+
+__device__ __forceinline__ uint32_t divide(unsigned long long n, unsigned long long d) {       // (quotients fit)
+  return (n | d) >> 32 ? (uint32_t)(n / d) : (uint32_t)n / (uint32_t)d;
+}
+
+template <int D, bool E4M3, int MB>
+struct Shape {
+  static constexpr int RT = 16 * MB;                     // rows of a tile
+  static constexpr int RB = E4M3 ? D : 2 * D;            // bytes of a cached row
+  static constexpr int LPR = RB / 16, RPI = 64 / LPR;    // lanes per row, rows of a load into LDS
+  static constexpr int NK = RB / 64;                     // 16-byte pieces of a row of K per lane
+  static constexpr int NS = D / 32, ND = D / 16;         // k-steps of the first product, column tiles of the second
+  static constexpr int kRing = 2 * 32 * RB;              // LDS bytes of a wavefront: two steps of V
+  static constexpr int OS = D + 4;                       // floats between rows where the wavefronts meet
+  static constexpr int kMerge = 4 * RT * OS * 4;
+  static constexpr int kLds = 4 * kRing > kMerge ? 4 * kRing : kMerge;
+  // 16-byte piece p of row r of V is kept at p ^ swizzle(r): the 32 lanes that a transposing read serves at once then touch all banks
+  __device__ static __forceinline__ int swizzle(int r) {
+    if (!E4M3) return RB == 256 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
+    return RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1;
+  }
+};
+
+// K of a step in registers, and the exponents of both.
+template <int NK>
+struct StepRegs {
+  u32x4 k[2][NK];
+  uint32_t ks[2], vs[2];
+};
+
+template <int D, bool E4M3, int MB>
+__global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
+  using S = Shape<D, E4M3, MB>;
+  constexpr int RT = S::RT, RB = S::RB;
+  __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
+  __shared__ float ml[4][RT][2];
+  __shared__ unsigned long long scan[4];
+  __shared__ unsigned long long place[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
+  const int n = a.b.n_seqs, Hkv = a.b.Hkv;
+
+  // ---- the share: thread t counts sequences t * per .. of the batch
+  unsigned long long total, share;
+  {
+    const int per = (n + 255) / 256;
+    unsigned long long mine = 0;
+    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += sequence<RT>(a, i).units(Hkv);
+    unsigned long long upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const unsigned long long o = __shfl_up(upto, m);
+      if (lane >= m) upto += o;
+    }
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) upto += scan[w];
+      total += scan[w];
+    }
+    share = (total + kShares - 1) / kShares;
+    const unsigned long long u0 = blockIdx.x * share;
+    unsigned long long at = upto - mine;
+    if (blockIdx.x == 0 || (u0 >= at && u0 < upto)) {
+      for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
+        const unsigned long long u = sequence<RT>(a, i).units(Hkv);
+        if (blockIdx.x == 0) a.before[i] = at;
+        if (u0 >= at && u0 < at + u) {
+          place[0] = i;
+          place[1] = u0 - at;
+        }
+        at += u;
+      }
+      if (blockIdx.x == 0 && tid == 0) a.before[n] = total;
+    }
+    if (u0 >= total) return;
+    __syncthreads();
+  }
+  unsigned long long u = blockIdx.x * share;
+  const unsigned long long end = u + share < total ? u + share : total;
+  int seq = (int)place[0];
+  unsigned long long in_seq = place[1];
+
+  const int lds0 = (int)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * S::kRing;
+  char* const ring = smem + wave * S::kRing;
+  // transposing reads: this lane's address in a step's V, up to the column tile (an exclusive or) and, in bf16, the second 16 keys
+  const int v_row = E4M3 ? 4 * quarter + ((lo >> 1) & 3) + ((lo >> 3) << 4) : 4 * quarter + (lo >> 2);
+  const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
+
+  while (u < end) {
+    Seq q = sequence<RT>(a, seq);
+    while (q.tiles == 0) q = sequence<RT>(a, ++seq);      // (u < total: there is one)
+    const uint32_t ht = divide(in_seq, q.steps), h = ht / q.tiles, tile = ht - h * q.tiles;
+    const int s0 = (int)(in_seq - (unsigned long long)ht * q.steps);
+    const int s1 = (int)(end - u < (unsigned long long)(q.steps - s0) ? s0 + (int)(end - u) : q.steps);
+
+    // ---- the rows
+    const int row0 = (int)tile * RT, pos0 = q.kv - q.q_len;
+    const int p_min = pos0 + (int)a.by_g.div(row0), p_max = pos0 + (int)a.by_g.div(min(row0 + RT, q.rows) - 1);
+    const int see_lo = a.window ? max(0, p_min - a.window + 1) : 0, see_hi = p_max + 1;     // keys that some row of the tile sees
+    const int all_lo = a.window ? p_max - a.window + 1 : 0;                                 // keys all_lo .. p_min are seen by all of them
+    bf16x8 qf[MB][S::NS];
+    int pos[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int r = min(row0 + 16 * mb + lo, q.rows - 1), tok = (int)a.by_g.div(r);
+      pos[mb] = pos0 + tok;
+      const __bf16* src = a.Q + (q.q0 + tok) * a.q_t + ((int)h * a.g + r - tok * a.g) * a.q_h;
+#pragma unroll
+      for (int st = 0; st < S::NS; ++st)
+        qf[mb][st] = *(const bf16x8*)(src + (E4M3 ? 64 * (st >> 1) + 16 * quarter + 8 * (st & 1) : 32 * st + 8 * quarter));
+    }
+
+    // ---- pages: lane l holds the id of the 16 keys from 16 (64 chunk + l) on, counted from q.first
+    auto page_ids = [&](int chunk) -> int {
+      const int key = q.first + 16 * (64 * chunk + lane);
+      return key < see_hi ? a.b.page(seq, key) : -1;
+    };
+    int chunk = s0 >> 3, ids = page_ids(chunk), ids_next = page_ids(chunk + 1);
+    auto issue = [&](int s, StepRegs<S::NK>& x, int buf) {
+      if ((s >> 3) != chunk) {
+        ++chunk;
+        ids = ids_next;
+        ids_next = page_ids(chunk + 1);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int id = __builtin_amdgcn_readlane(ids, (8 * s + 2 * wave + j) & 63);
+        const int key0 = q.first + 16 * (8 * s + 2 * wave + j);
+        const long long row = a.b.row(max(id, 0), (int)h, key0);
+        const char* kr = a.kp + (row + lo) * RB + 16 * quarter;
+#pragma unroll
+        for (int i = 0; i < S::NK; ++i) x.k[j][i] = *(const u32x4*)(kr + 64 * i);
+        if (E4M3) {
+          x.ks[j] = a.ks[row + lo];
+          x.vs[j] = *(const uint32_t*)(a.vs + row + 4 * quarter);
+        }
+#pragma unroll
+        for (int i = 0; i < 16 / S::RPI; ++i) {
+          const int r = i * S::RPI + lane / S::LPR, piece = (lane % S::LPR) ^ S::swizzle(16 * j + r);
+          const bool seen = id >= 0 && key0 + r >= see_lo && key0 + r < see_hi;
+          load_row_to_lds((seen ? a.vp + (row + r) * RB : (const char*)g_zeros) + 16 * piece, lds0 + buf * (32 * RB) + (16 * j + i * S::RPI) * RB);
+        }
+      }
+    };
+
+    f32x4 o[MB][S::ND];
+    float m[MB], l[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      m[mb] = kNone;
+      l[mb] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < S::ND; ++dt) o[mb][dt] = f32x4{0, 0, 0, 0};
+    }
+
+    auto compute = [&](int s, int ids_s, const StepRegs<S::NK>& x, int buf) {
+      const int key0 = q.first + 16 * (8 * s + 2 * wave);
+      bool masked[2], dead[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int k0 = key0 + 16 * j;
+        const bool gone = __builtin_amdgcn_readlane(ids_s, (8 * s + 2 * wave + j) & 63) < 0;
+        dead[j] = gone || k0 >= see_hi || k0 + 15 < see_lo;
+        masked[j] = dead[j] || k0 + 15 > p_min || k0 < all_lo;
+      }
+      if (dead[0] && dead[1]) return;
+      f32x4 sc[MB][2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) sc[mb][j] = f32x4{0, 0, 0, 0};
+        const float k_scale = E4M3 ? exponent_value(x.ks[j]) : 1.0f;
+#pragma unroll
+        for (int st = 0; st < S::NS; ++st) {
+          bf16x8 kf;
+          if (E4M3) kf = widen8(x.k[j][st >> 1][2 * (st & 1)], x.k[j][st >> 1][2 * (st & 1) + 1], k_scale);
+          else kf = __builtin_bit_cast(bf16x8, x.k[j][st]);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) sc[mb][j] = mfma16(kf, qf[mb][st], sc[mb][j]);
+        }
+        if (masked[j]) {
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int key = key0 + 16 * j + 4 * quarter + r;
+              if (dead[j] || key > pos[mb] || (a.window && key <= pos[mb] - a.window)) sc[mb][j][r] = -INFINITY;
+            }
+        }
+      }
+      bf16x8 pf[MB];
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        float mx = sc[mb][0][0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, sc[mb][r >> 2][r & 3]);
+        mx *= a.c;
+        if (__any(mx > m[mb] + kLag)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float mn = fmaxf(m[mb], mx), alpha = fast_exp2(m[mb] - mn);
+          m[mb] = mn;
+          l[mb] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[mb][dt][r] *= alpha;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = fast_exp2(fmaf(sc[mb][j][r], a.c, -m[mb]));
+            l[mb] += p;
+            // (bf16 for the product, as the other attention kernels have it; V's power of two is exact.  A byte of a row that nobody
+            // has written may say infinity, next to a probability of 0.)
+            pf[mb][4 * j + r] = (__bf16)(E4M3 ? p * fminf(exponent_value((x.vs[j] >> (8 * r)) & 0xffu), 0x1p127f) : p);
+          }
+      }
+#pragma unroll
+      for (int dt = 0; dt < S::ND; ++dt) {
+        bf16x8 vf;
+        if (E4M3) {
+          typedef __attribute__((ext_vector_type(2))) int i32x2;
+          const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(ring + buf * (32 * RB) + (v_rd ^ (dt << 4))));
+          vf = widen8((uint32_t)w[0], (uint32_t)w[1], 1.0f);
+        } else {
+          const char* at = ring + buf * (32 * RB) + (v_rd ^ (dt << 5));
+          const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)at);
+          const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at + 16 * RB));
+          vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) o[mb][dt] = mfma16(vf, pf[mb], o[mb][dt]);
+      }
+    };
+
+    StepRegs<S::NK> xa, xb;
+    issue(s0, xa, 0);
+    for (int s = s0;; s += 2) {
+      wait_all();
+      int ids_s = ids;
+      if (s + 1 < s1) issue(s + 1, xb, 1);
+      compute(s, ids_s, xa, 0);
+      if (s + 1 >= s1) break;
+      wait_all();
+      ids_s = ids;
+      if (s + 2 < s1) issue(s + 2, xa, 0);
+      compute(s + 1, ids_s, xb, 1);
+      if (s + 2 >= s1) break;
+    }
+
+    // ---- the four wavefronts meet
+    __syncthreads();                                     // (the rings are free)
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      l[mb] += __shfl_xor(l[mb], 16);
+      l[mb] += __shfl_xor(l[mb], 32);
+      if (quarter == 0) {
+        ml[wave][16 * mb + lo][0] = m[mb];
+        ml[wave][16 * mb + lo][1] = l[mb];
+      }
+    }
+    __syncthreads();
+    float* const meet = (float*)smem;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int r = 16 * mb + lo;
+      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0])), alpha = fast_exp2(m[mb] - mt);
+#pragma unroll
+      for (int dt = 0; dt < S::ND; ++dt) *(f32x4*)(meet + (wave * RT + r) * S::OS + 16 * dt + 4 * quarter) = o[mb][dt] * alpha;
+    }
+    __syncthreads();
+    const bool whole = s0 == 0 && s1 == q.steps;
+    const long long slot = 2LL * blockIdx.x + (s0 == 0 ? 1 : 0);
+    for (int task = tid; task < RT * (D / 8); task += 256) {
+      const int r = task / (D / 8), col = 8 * (task % (D / 8));
+      if (row0 + r >= q.rows) continue;
+      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0]));
+      float lt = 0.f;
+      f32x4 v[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        lt += ml[w][r][1] * fast_exp2(ml[w][r][0] - mt);
+        v[0] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col);
+        v[1] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col + 4);
+      }
+      if (whole) {
+        const int tok = (int)a.by_g.div(row0 + r), head = (int)h * a.g + row0 + r - tok * a.g;
+        const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+        bf16x8 out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (__bf16)(v[i >> 2][i & 3] * inv);
+        *(bf16x8*)(a.O + (q.q0 + tok) * a.o_t + head * a.o_h + col) = out;
+        if (a.lse && col == 0) a.lse[(long long)(q.q0 + tok) * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+      } else {
+        float* dst = a.part_o + (slot * RT + r) * D + col;
+        *(f32x4*)dst = v[0];
+        *(f32x4*)(dst + 4) = v[1];
+        if (col == 0) {
+          a.part_ml[(slot * RT + r) * 2] = mt;
+          a.part_ml[(slot * RT + r) * 2 + 1] = lt;
+        }
+      }
+    }
+    __syncthreads();
+    u += s1 - s0;
+    in_seq += s1 - s0;
+    if (in_seq >= q.units(Hkv)) {
+      ++seq;
+      in_seq = 0;
+    }
+  }
+}
+
+// Joins the parts of the rows that no share had whole: one workgroup per token and query head, the parts dealt over its wavefronts.
+// A row tile's first part is the second slot of its share, every later one the first slot of its share.
+template <int D, int RT>
+__global__ __launch_bounds__(256) void attend_join(Args a) {
+  __shared__ float meet[4][D];
+  __shared__ float ml[4][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int t = blockIdx.x, head = blockIdx.y, h = (int)a.by_g.div(head);
+  const int seq = sequence_of(a.b, t, lane);
+  if (seq < 0 || seq >= a.b.n_seqs) return;
+  const Seq q = sequence<RT>(a, seq);
+  if (t < q.q0 || t >= q.q0 + q.q_len) return;
+  const unsigned long long total = a.before[a.b.n_seqs], share = (total + kShares - 1) / kShares;
+  const int r = (t - q.q0) * a.g + head - h * a.g, tile = r / RT;
+  const unsigned long long u0 = a.before[seq] + ((unsigned long long)h * q.tiles + tile) * q.steps, u1 = u0 + q.steps;
+  const int w0 = (int)divide(u0, share), w1 = (int)divide(u1 - 1, share);
+  if (w0 == w1) return;
+  const int in_tile = r - tile * RT;
+  constexpr int N = D / 64;
+  float m = kNone, l = 0.f, o[N] = {};
+  for (int w = w0 + wave; w <= w1; w += 4) {
+    const long long slot = (2LL * w + (w == w0 ? 1 : 0)) * RT + in_tile;
+    const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1];
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = a.part_o[slot * D + N * lane + i];
+    const float mn = fmaxf(m, mp), x = fast_exp2(m - mn), y = fast_exp2(mp - mn);
+    m = mn;
+    l = l * x + lp * y;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = o[i] * x + v[i] * y;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) meet[wave][N * lane + i] = o[i];
+  if (lane == 0) {
+    ml[wave][0] = m;
+    ml[wave][1] = l;
+  }
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  const float mt = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+  float lt = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float x = fast_exp2(ml[w][0] - mt);
+    lt += ml[w][1] * x;
+    v0 += meet[w][2 * threadIdx.x] * x;
+    v1 += meet[w][2 * threadIdx.x + 1] * x;
+  }
+  const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+  bf16x2 out;
+  out[0] = (__bf16)(v0 * inv);
+  out[1] = (__bf16)(v1 * inv);
+  *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + 2 * threadIdx.x) = out;
+  if (a.lse && threadIdx.x == 0) a.lse[(long long)t * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+template <int D, bool E4M3>
+hipError_t launch(const Args& a, hipStream_t st) {
+  attend_few_rows<D, E4M3, 1><<<kShares, 256, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  attend_join<D, 16><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attend_cache_ws_bytes(const CacheArgs& c) {
+  return align256((size_t)(c.n_seqs + 1) * 8) + align256(2 * (size_t)kShares * 16 * 2 * 4) + align256(2 * (size_t)kShares * 16 * c.d * 4);
+}
+
+hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float* lse, void* ws, hipStream_t st) {
+  Args a;
+  a.b.cu_q = c.cu_q; a.b.kv_len = c.kv_len; a.b.table = c.table;
+  a.b.n_seqs = c.n_seqs; a.b.n_tokens = c.n_tokens; a.b.max_pages = c.max_pages; a.b.page_log2 = c.page_log2; a.b.n_pages = c.n_pages; a.b.Hkv = c.Hkv;
+  a.Q = (const __bf16*)Q; a.kp = (const char*)c.kp; a.vp = (const char*)c.vp; a.ks = (const uint8_t*)c.ks; a.vs = (const uint8_t*)c.vs;
+  a.O = (__bf16*)O; a.lse = lse;
+  a.q_t = c.q_t; a.q_h = c.q_h; a.o_t = c.o_t; a.o_h = c.o_h;
+  a.Hq = c.Hq; a.g = c.Hq / c.Hkv; a.window = c.window; a.c = c.scale * kLog2e;
+  a.by_g = FastDiv((uint32_t)a.g, (uint64_t)c.n_tokens * a.g + 1);
+  char* base = (char*)ws;
+  a.before = (unsigned long long*)base;
+  base += align256((size_t)(c.n_seqs + 1) * 8);
+  a.part_ml = (float*)base;
+  base += align256(2 * (size_t)kShares * 16 * 2 * 4);
+  a.part_o = (float*)base;
+  if (c.d == 128) return c.e4m3 ? launch<128, true>(a, st) : launch<128, false>(a, st);
+  return c.e4m3 ? launch<64, true>(a, st) : launch<64, false>(a, st);
+}
+
+}  // namespace tsa

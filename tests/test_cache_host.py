@@ -84,3 +84,28 @@ def test_refused():
     d = _desc(n_tokens=2, n_seqs=1)
     with pytest.raises(tsa.TsaError):
         tsa.tsa_cache_write(d, torch.zeros(2, 2, 64, dtype=torch.bfloat16), None, None, None, None, None, None)      # not on a GPU
+
+
+def _attend(desc, Q=FAKE, kp=FAKE, vp=FAKE, ks=None, vs=None, cu=FAKE, kv=FAKE, tab=FAKE, O=FAKE, lse=None, ws=FAKE, n=1 << 40):
+    return tsa.load_library().tsa_attend_cache(ctypes.byref(desc) if desc is not None else None, Q, kp, vp, ks, vs, cu, kv, tab, O, lse, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,rc", BAD_DESCS)
+def test_attend_bad_descriptors(kw, rc):
+    assert _attend(_desc(**kw)) == rc
+    assert tsa.load_library().tsa_attend_cache_workspace_bytes(ctypes.byref(_desc(**kw))) == 0
+
+
+def test_attend_refused():
+    arg, small = tsa.TSA_ERR_ARG, tsa.TSA_ERR_WORKSPACE
+    assert _attend(None) == arg
+    d, e = _desc(), _desc(format=tsa.TSA_CACHE_E4M3)
+    for name in ("Q", "kp", "vp", "cu", "kv", "tab", "O"):
+        assert _attend(d, **{name: None}) == arg and _attend(d, **{name: ODD4}) == arg, name
+    assert _attend(d, lse=ODD4) == arg and _attend(e) == arg and _attend(e, ks=FAKE) == arg and _attend(d, vs=FAKE) == arg
+    need = tsa.load_library().tsa_attend_cache_workspace_bytes(ctypes.byref(d))
+    assert need > 0 and _attend(d, n=need - 1) == small and _attend(d, ws=None) == small and _attend(d, ws=ctypes.c_void_p(0x1080)) == small
+    assert _attend(_desc(n_tokens=1 << 22, Hq=1024, Hkv=1)) == tsa.TSA_ERR_UNSUPPORTED
+    assert _attend(_desc(n_tokens=0), Q=None, O=None, ws=None, n=0) == tsa.TSA_OK
+    with pytest.raises(tsa.TsaError):
+        tsa.alloc_attend_cache_workspace(_desc(d=80))

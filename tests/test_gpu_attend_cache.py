@@ -1,0 +1,248 @@
+"""tsa_attend_cache against the oracle in 64 bits: single tokens, drafted tokens, prompts and all of them mixed, both formats, every page
+size, groups of heads, windows, pages that are not there, tokens that see nothing, garbage where nobody looks."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving_oracle as srv
+from oracle import tsa_oracle as orc
+from tests import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tsa():
+    from paper_2602_03216_amd import binding
+    binding.load_library(build_if_missing=False)
+    return binding
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device=gu.DEV)
+
+
+class Batch:
+    """A ragged batch, its cache (NaN, and exponents of infinity, in every place that no sequence has) and what the oracle says."""
+
+    def __init__(self, seed, new, kv, Hq, Hkv, d, page, e4m3=0, window=0, pad=0, gone=(), spread=1.0, scale=0.0):
+        r = np.random.Generator(np.random.PCG64(seed))
+        self.new, self.kv, self.Hq, self.Hkv, self.d, self.page, self.e4m3, self.window = new, kv, Hq, Hkv, d, page, e4m3, window
+        n = len(new)
+        self.cu = np.concatenate([[0], np.cumsum(new)])
+        self.T = sum(new) + pad
+        need = [-(-k // page) for k in kv]
+        self.max_pages = max(1, max(need))
+        self.n_pages = sum(need) + 2
+        ids = r.permutation(self.n_pages)
+        self.tab = np.full((n, self.max_pages), -1, dtype=np.int64)
+        shape = (self.n_pages, Hkv, page, d)
+        pools = [np.full(shape, 0x7f if e4m3 else 0x7fc0, dtype=np.uint8 if e4m3 else np.uint16) for _ in "kv"]
+        scales = [np.full(shape[:3], 255, dtype=np.uint8) for _ in "kv"]
+        self.rows = []                                   # per sequence: K, V [Hkv, L, d] in float64, there [L]
+        at = 0
+        for i in range(n):
+            self.tab[i, :need[i]] = ids[at:at + need[i]]
+            at += need[i]
+            bits = [gu.rand_bits(r, (Hkv, kv[i], d), s) for s in (spread, 1.0)]
+            both = []
+            for w in (0, 1):
+                code, byte = srv.quantise_rows(bits[w]) if e4m3 and kv[i] else (bits[w], None)
+                for p in range(need[i]):
+                    cut = slice(p * page, min(kv[i], (p + 1) * page))
+                    pools[w][self.tab[i, p], :, :cut.stop - cut.start] = code[:, cut]
+                    if e4m3:
+                        scales[w][self.tab[i, p], :, :cut.stop - cut.start] = byte[:, cut]
+                both.append(srv.e4m3_value(code) * 2.0 ** (byte[..., None].astype(float) - 127) if byte is not None else orc.bf16_to_f64(bits[w]))
+            there = np.ones(kv[i], dtype=bool)
+            for s, p in gone:
+                if s == i and p < need[i]:
+                    self.tab[i, p] = [-1, self.n_pages, -7, 1 << 30][p % 4]
+                    there[p * page:(p + 1) * page] = False
+            self.rows.append((both[0], both[1], there))
+        self.q = gu.rand_bits(r, (self.T, Hq, d))
+        self.pools = [torch.from_numpy(p if e4m3 else p.view(np.int16)).to(gu.DEV) for p in pools]
+        if not e4m3:
+            self.pools = [p.view(torch.bfloat16) for p in self.pools]
+        self.scales = [torch.from_numpy(s).to(gu.DEV) if e4m3 else None for s in scales]
+        self.scale = scale
+
+    def desc(self, tsa, **kw):
+        return tsa.make_cache_desc(len(self.new), self.T, self.Hq, self.Hkv, self.d, self.page, self.n_pages, self.max_pages,
+                                   tsa.TSA_CACHE_E4M3 if self.e4m3 else tsa.TSA_CACHE_BF16, **dict(dict(max_q=max(self.new), window=self.window, scale=self.scale), **kw))
+
+    def run(self, tsa, ws=None, Q=None, O=None, **kw):
+        desc = self.desc(tsa, **kw)
+        if ws is None:
+            ws = tsa.alloc_attend_cache_workspace(desc)
+            ws.fill_(0xff)
+        Q = gu.to_dev(self.q) if Q is None else Q
+        O = torch.full((self.T, self.Hq, self.d), 7.0, dtype=torch.bfloat16, device=gu.DEV) if O is None else O
+        lse = torch.full((self.T, self.Hq), 7.0, device=gu.DEV)
+        tsa.tsa_attend_cache(desc, Q, *self.pools, ints(self.cu), ints(self.kv), ints(self.tab), O, ws, lse=lse, k_scales=self.scales[0], v_scales=self.scales[1])
+        return O, lse
+
+    def check(self, O, lse):
+        """Probabilities and output rounded to bf16, half a step each (2^-8 of the average of |v|, 2^-8 of the output); sums of up to 128 products
+        in 32 bits move a logit by less than 2^-13 here, which moves a probability by as much."""
+        got, lse = orc.bf16_to_f64(gu.from_dev(O)), lse.double().cpu().numpy()
+        g, q = self.Hq // self.Hkv, orc.bf16_to_f64(self.q)
+        scale = self.scale or self.d ** -0.5
+        for i in range(len(self.new)):
+            n, cut = self.new[i], slice(self.cu[i], self.cu[i + 1])
+            if n == 0:
+                continue
+            K, V, there = self.rows[i]
+            for h in range(self.Hq):
+                qh = q[cut, h]
+                first = max(0, n - self.kv[i])           # tokens at negative positions
+                want, ref, mag = (np.zeros((n, self.d)), np.full(n, -np.inf), np.zeros((n, self.d)))
+                if self.kv[i]:
+                    want[first:], ref[first:], mag[first:] = srv.attend(qh[first:], K[h // g], V[h // g], there, scale, self.window)
+                err = np.abs(got[cut, h] - want)
+                tol = (2.0 ** -8 + 2.0 ** -12) * mag + 2.0 ** -8 * np.abs(want) + 1e-30
+                assert (err <= tol).all(), "sequence %d head %d: %.3g of the tolerance" % (i, h, (err / tol).max())
+                seen = np.isfinite(ref)
+                assert np.array_equal(seen, np.isfinite(lse[cut, h])) and (lse[cut, h][~seen] == -np.inf).all()
+                assert (got[cut, h][~seen] == 0).all()
+                assert (np.abs(lse[cut, h][seen] - ref[seen]) <= 2.0 ** -12 + 2.0 ** -22 * np.abs(ref[seen])).all(), "sequence %d head %d" % (i, h)
+        if self.T > self.cu[-1]:
+            assert (got[self.cu[-1]:] == 7).all() and (lse[self.cu[-1]:] == 7).all()
+
+
+CASES = {
+    "one_token_one_key": dict(new=[1], kv=[1], Hq=1, Hkv=1, d=64, page=16),
+    "one_token": dict(new=[1], kv=[701], Hq=32, Hkv=8, d=128, page=16),
+    "ends_inside_tiles": dict(new=[1] * 9, kv=[15, 16, 17, 127, 128, 129, 255, 257, 1000], Hq=8, Hkv=2, d=128, page=16),
+    "empty_sequences": dict(new=[0, 1, 0, 0, 2, 0], kv=[5, 300, 0, 40, 90, 0], Hq=4, Hkv=4, d=64, page=32, pad=3),
+    "no_cache_at_all": dict(new=[1, 3], kv=[0, 0], Hq=4, Hkv=2, d=128, page=16),
+    "more_new_than_cached": dict(new=[5, 40], kv=[2, 33], Hq=6, Hkv=2, d=64, page=64, pad=1),
+    "seven_heads": dict(new=[3, 5, 1], kv=[300, 5, 77], Hq=28, Hkv=4, d=128, page=16),
+    "forty_heads_one_kv": dict(new=[1, 2], kv=[130, 515], Hq=40, Hkv=1, d=64, page=128),
+    "window": dict(new=[1, 4, 2, 1], kv=[2000, 700, 3, 129], Hq=8, Hkv=2, d=128, page=16, window=128),
+    "window_of_one": dict(new=[3, 1], kv=[50, 1], Hq=4, Hkv=2, d=64, page=16, window=1),
+    "window_odd": dict(new=[7, 20], kv=[999, 321], Hq=4, Hkv=1, d=64, page=32, window=77),
+    "pages_gone": dict(new=[2, 1, 3], kv=[400, 64, 130], Hq=8, Hkv=4, d=128, page=32, gone=[(0, 1), (0, 5), (1, 0), (1, 1), (2, 4), (2, 0)]),
+    "window_and_pages_gone": dict(new=[4], kv=[1500], Hq=8, Hkv=2, d=128, page=16, window=200, gone=[(0, p) for p in range(81)]),
+    "long": dict(new=[1, 2], kv=[20000, 9001], Hq=8, Hkv=2, d=128, page=256),
+    "many_short": dict(new=[1] * 300, kv=list(range(1, 301)), Hq=4, Hkv=2, d=64, page=16),
+    "large_logits": dict(new=[2, 1], kv=[600, 31], Hq=4, Hkv=2, d=64, page=16, scale=1.5),
+    "prompt": dict(new=[200], kv=[200], Hq=8, Hkv=2, d=128, page=16),
+    "piece_of_a_prompt": dict(new=[333], kv=[1111], Hq=4, Hkv=4, d=64, page=64),
+    "mixed": dict(new=[1, 150, 0, 1, 257, 9], kv=[900, 150, 70, 33, 600, 9], Hq=8, Hkv=2, d=128, page=32, pad=2),
+    "mixed_window": dict(new=[1, 300, 130], kv=[900, 300, 777], Hq=6, Hkv=2, d=64, page=16, window=100),
+    "mixed_gone": dict(new=[1, 140, 130], kv=[900, 140, 777], Hq=6, Hkv=2, d=128, page=32, gone=[(0, 3), (1, 0), (1, 2), (2, 11), (2, 24)]),
+}
+
+
+@pytest.mark.parametrize("e4m3", [0, 1])
+@pytest.mark.parametrize("name", list(CASES))
+def test_against_the_oracle(tsa, name, e4m3):
+    b = Batch(6000 + list(CASES).index(name), e4m3=e4m3, **CASES[name])
+    b.check(*b.run(tsa))
+
+
+@pytest.mark.parametrize("e4m3,d,page", [(0, 128, 64), (1, 128, 128), (0, 64, 256), (1, 64, 32)])
+@pytest.mark.parametrize("seed", range(3))
+def test_random_batches(tsa, seed, e4m3, d, page):
+    r = np.random.Generator(np.random.PCG64(6500 + 10 * seed + d + e4m3))
+    n = int(r.integers(1, 12))
+    new = [int(r.choice([0, 1, 1, 1, 2, 5, int(r.integers(1, 300))])) for _ in range(n)]
+    if not sum(new):
+        new[0] = 1
+    kv = [int(x + r.integers(0, 1500)) for x in new]
+    Hq, Hkv = [(4, 4), (12, 4), (16, 2), (28, 4), (8, 1)][int(r.integers(5))]
+    b = Batch(6600 + seed, new, kv, Hq, Hkv, d, page, e4m3, window=int(r.choice([0, 0, 50, 400])), pad=int(r.integers(0, 3)))
+    b.check(*b.run(tsa))
+
+
+@pytest.mark.parametrize("name", ["one_token", "mixed", "window", "more_new_than_cached"])
+def test_what_the_caller_knows_does_not_change_what_is_computed(tsa, name):
+    """Any max_q, another workspace: right all the same; the same call twice: the same bits."""
+    b = Batch(6700, **CASES[name])
+    first = b.run(tsa)
+    again = b.run(tsa)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    for max_q in (0, 1, 1000):
+        b.check(*b.run(tsa, max_q=max_q))
+
+
+@pytest.mark.parametrize("name", ["seven_heads", "mixed"])
+def test_strides(tsa, name):
+    """Q out of the rows of a projection, O into rows with room between them, heads first."""
+    b = Batch(6800, **CASES[name])
+    T, Hq, d = b.T, b.Hq, b.d
+    want, lse = b.run(tsa)
+    wide = torch.zeros(T, (Hq + 6) * d, dtype=torch.bfloat16, device=gu.DEV)
+    Q = wide[:, 2 * d:(Hq + 2) * d].unflatten(-1, (Hq, d))
+    Q.copy_(gu.to_dev(b.q))
+    out = torch.full((Hq, T, d + 8), 7.0, dtype=torch.bfloat16, device=gu.DEV)
+    O = out[:, :, :d].transpose(0, 1)
+    _, lse2 = b.run(tsa, Q=Q, O=O, q_strides=Q.stride()[:2], o_strides=O.stride()[:2])
+    assert torch.equal(O.contiguous(), want) and torch.equal(lse, lse2) and (out[..., d:] == 7).all()
+
+
+def test_without_lse_and_on_another_stream(tsa):
+    b = Batch(6900, **CASES["mixed"])
+    want, _ = b.run(tsa)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    desc = b.desc(tsa)
+    Q, O, ws = gu.to_dev(b.q), torch.full_like(want, 7.0), tsa.alloc_attend_cache_workspace(desc)
+    args = ints(b.cu), ints(b.kv), ints(b.tab)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        tsa.tsa_attend_cache(desc, Q, *b.pools, *args, O, ws)
+    st.synchronize()
+    assert torch.equal(O, want)
+
+
+def test_captured(tsa):
+    """One graph for steps of any lengths: two graphs share a workspace, lengths and tables change between the replays."""
+    Hq, Hkv, d, page, n = 8, 2, 128, 16, 3
+    batches = [Batch(7000 + k, [1, 1, 1], kv, Hq, Hkv, d, page) for k, kv in enumerate([[100, 7, 40], [1500, 3, 900], [5, 2000, 16]])]
+    n_pages, max_pages = max(b.n_pages for b in batches), max(b.max_pages for b in batches)
+    desc = tsa.make_cache_desc(n, 3, Hq, Hkv, d, page, n_pages, max_pages)
+    new = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device=gu.DEV)
+    Q, O, kp, vp = new(3, Hq, d), new(3, Hq, d), new(n_pages, Hkv, page, d), new(n_pages, Hkv, page, d)
+    cu, kv, tab, ws = ints([0, 1, 2, 3]), ints([1, 1, 1]), ints(np.zeros((n, max_pages))), tsa.alloc_attend_cache_workspace(desc)
+    lse = new(3, Hq, dtype=torch.float32)
+    step = lambda: tsa.tsa_attend_cache(desc, Q, kp, vp, cu, kv, tab, O, ws, lse=lse)
+    step()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append(g)
+    for k in range(6):
+        b = batches[k % 3]
+        Q.copy_(gu.to_dev(b.q))
+        kp[:b.n_pages].copy_(b.pools[0])
+        vp[:b.n_pages].copy_(b.pools[1])
+        kv.copy_(ints(b.kv))
+        tab.fill_(-1)
+        tab[:, :b.max_pages].copy_(ints(b.tab))
+        O.fill_(7.0)
+        graphs[k % 2].replay()
+        torch.cuda.synchronize()
+        b.check(O, lse)
+
+
+def test_a_pool_beyond_four_gigabytes(tsa):
+    """Pages whose place does not fit 32 bits, in one sequence with pages that do."""
+    H, d, page, n_pages, kv = 8, 128, 256, 9000, 1000
+    r = np.random.Generator(np.random.PCG64(7100))
+    kp, vp = (torch.zeros(n_pages, H, page, d, dtype=torch.bfloat16, device=gu.DEV) for _ in "kv")
+    tab = [[8999, 1, 8500, 4000]]
+    K, V, Q = gu.rand_bits(r, (kv, H, d)), gu.rand_bits(r, (kv, H, d)), gu.rand_bits(r, (3, 2 * H, d))
+    desc = tsa.make_cache_desc(1, kv, H, H, d, page, n_pages, 4)
+    tsa.tsa_cache_write(desc, gu.to_dev(K), gu.to_dev(V), ints([0, kv]), ints([kv]), ints(tab), kp, vp)
+    desc = tsa.make_cache_desc(1, 3, 2 * H, H, d, page, n_pages, 4)
+    O = torch.zeros(3, 2 * H, d, dtype=torch.bfloat16, device=gu.DEV)
+    tsa.tsa_attend_cache(desc, gu.to_dev(Q), kp, vp, ints([0, 3]), ints([kv]), ints(tab), O, tsa.alloc_attend_cache_workspace(desc))
+    got, q = orc.bf16_to_f64(gu.from_dev(O)), orc.bf16_to_f64(Q)
+    for h in range(2 * H):
+        want, _, mag = srv.attend(q[:, h], orc.bf16_to_f64(K[:, h // 2]), orc.bf16_to_f64(V[:, h // 2]), np.ones(kv, dtype=bool), d ** -0.5)
+        assert (np.abs(got[:, h] - want) <= (2.0 ** -8 + 2.0 ** -12) * mag + 2.0 ** -8 * np.abs(want)).all()
