@@ -17,65 +17,16 @@
 // next step's K and V are in flight while a step is computed, and no wavefront waits for another inside a segment.
 //   8 bits: K is widened to bf16 with its row's power of two by the conversion (exact), V without it, and V's power goes into the
 // probability in front of its rounding.
-#include "cache_common.h"
+#include "attend_cache.h"
 
 namespace tsa {
 
 using namespace cache_detail;
+using namespace attend_cache_detail;
 
 namespace {
 
-constexpr float kNone = -1.0e30f;                        // running max of a row that has seen no key
-constexpr float kLag = 8.0f;                             // log2 units that the running max may lag behind
-constexpr int kStep = 128;                               // keys of a step
-constexpr int kShares = 512;                             // workgroups: two per CU
-
-struct Args {
-  Batch b;
-  const __bf16* Q;
-  const char* kp;
-  const char* vp;
-  const uint8_t* ks;
-  const uint8_t* vs;
-  __bf16* O;
-  float* lse;
-  long long q_t, q_h, o_t, o_h;
-  int Hq, g, window;
-  float c;                       // scale * log2(e)
-  FastDiv by_g;
-  // workspace
-  unsigned long long* before;    // [n_seqs + 1] steps in front of every sequence
-  float* part_o;                 // [2 kShares][RT][d]
-  float* part_ml;                // [2 kShares][RT][2]
-};
-
-__device__ const u32x4 g_zeros[16] = {};                 // a row of V for keys that nobody sees
-
-// 64 lanes' 16 bytes to LDS bytes lds .. lds + 1023.  Counted by vmcnt and by nothing that the compiler tracks; no output register.  The wait
-// states: m0 may come out of a vector instruction.
-__device__ __forceinline__ void load_row_to_lds(const void* p, int lds) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  lds = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
-#endif
-}
-// Everything that this wavefront asked for has landed, in registers and in LDS, and its LDS reads are done.
-__device__ __forceinline__ void wait_all() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0070);
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
-  u32x4 w;
-  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
-  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
-  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
-  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
-  return __builtin_bit_cast(bf16x8, w);
-}
 
 // What a sequence asks for.
 struct Seq {
@@ -90,6 +41,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int i) {
   s.q_len = max(a.b.first(i + 1) - s.q0, 0);
   s.kv = a.b.kv(i);
   s.rows = s.q_len * a.g;
+  if (s.rows > a.few) s.rows = 0;
   s.tiles = (s.rows + RT - 1) / RT;
   s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
   s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
@@ -423,20 +375,40 @@ __global__ __launch_bounds__(256) void attend_join(Args a) {
   if (seq < 0 || seq >= a.b.n_seqs) return;
   const Seq q = sequence<RT>(a, seq);
   if (t < q.q0 || t >= q.q0 + q.q_len) return;
-  const unsigned long long total = a.before[a.b.n_seqs], share = (total + kShares - 1) / kShares;
-  const int r = (t - q.q0) * a.g + head - h * a.g, tile = r / RT;
-  const unsigned long long u0 = a.before[seq] + ((unsigned long long)h * q.tiles + tile) * q.steps, u1 = u0 + q.steps;
-  const int w0 = (int)divide(u0, share), w1 = (int)divide(u1 - 1, share);
-  if (w0 == w1) return;
-  const int in_tile = r - tile * RT;
+  const int r = (t - q.q0) * a.g + head - h * a.g;
+  // parts 0 .. parts - 1: row `first` of the slots, then `next`, `next` + every, ..
+  const float *part_o, *part_ml;
+  long long first, next;
+  int parts, every;
+  if (q.rows == 0) {                                     // many rows
+    const ManyTile x = many_tile(a, seq, r / kManyRows);
+    parts = x.parts;
+    first = (((long long)first_slot(a, seq) + r / kManyRows) * a.b.Hkv + h) * a.splits * kManyRows + r % kManyRows;
+    every = kManyRows;
+    next = first + every;
+    part_o = a.many_o;
+    part_ml = a.many_ml;
+  } else {
+    const unsigned long long total = a.before[a.b.n_seqs], share = (total + kShares - 1) / kShares;
+    const int tile = r / RT;
+    const unsigned long long u0 = a.before[seq] + ((unsigned long long)h * q.tiles + tile) * q.steps, u1 = u0 + q.steps;
+    const int w0 = (int)divide(u0, share), w1 = (int)divide(u1 - 1, share);
+    parts = w1 - w0 + 1;
+    first = (2LL * w0 + 1) * RT + r - tile * RT;
+    every = 2 * RT;
+    next = first + RT;
+    part_o = a.part_o;
+    part_ml = a.part_ml;
+  }
+  if (parts == 1) return;
   constexpr int N = D / 64;
   float m = kNone, l = 0.f, o[N] = {};
-  for (int w = w0 + wave; w <= w1; w += 4) {
-    const long long slot = (2LL * w + (w == w0 ? 1 : 0)) * RT + in_tile;
-    const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1];
+  for (int w = wave; w < parts; w += 4) {
+    const long long slot = w == 0 ? first : next + (long long)(w - 1) * every;
+    const float mp = part_ml[2 * slot], lp = part_ml[2 * slot + 1];
     float v[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = a.part_o[slot * D + N * lane + i];
+    for (int i = 0; i < N; ++i) v[i] = part_o[slot * D + N * lane + i];
     const float mn = fmaxf(m, mp), x = fast_exp2(m - mn), y = fast_exp2(mp - mn);
     m = mn;
     l = l * x + lp * y;
@@ -470,20 +442,66 @@ __global__ __launch_bounds__(256) void attend_join(Args a) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Sequences with at most this many rows (new tokens times heads of a group) are dealt by keys, the others by rows.
+constexpr int kFewRows = 32;
+
+// How a call is cut, from what the host knows: whether any sequence may have many rows, the slots for row tiles, and into how many parts
+// their keys are cut so that 512 workgroups run.
+struct Plan {
+  bool few, many;
+  int slots, splits;
+};
+Plan plan_of(const CacheArgs& c) {
+  const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
+  Plan p;
+  p.many = (long long)most * g > kFewRows;
+  p.few = !p.many || c.n_seqs > 1;
+  p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
+  const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
+  const long long keys = (long long)c.max_pages << c.page_log2, most_parts = keys / (kTile * kPartTiles);
+  long long s = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
+  if (s > most_parts) s = most_parts;
+  p.splits = s < 1 ? 1 : (int)s;
+  return p;
+}
+
+struct Workspace {
+  size_t part_ml, part_o, many_ml, many_o, total;
+};
+Workspace workspace_of(const CacheArgs& c, const Plan& p) {
+  Workspace w;
+  size_t at = align256((size_t)(c.n_seqs + 1) * 8);
+  auto take = [&](size_t n) { const size_t x = at; at += align256(n); return x; };
+  w.part_ml = take(2 * (size_t)kShares * 16 * 2 * 4);
+  w.part_o = take(2 * (size_t)kShares * 16 * c.d * 4);
+  const size_t rows = p.many && p.splits > 1 ? (size_t)p.slots * c.Hkv * p.splits * kManyRows : 0;
+  w.many_ml = take(rows * 2 * 4);
+  w.many_o = take(rows * c.d * 4);
+  w.total = at;
+  return w;
+}
+
 template <int D, bool E4M3>
-hipError_t launch(const Args& a, hipStream_t st) {
-  attend_few_rows<D, E4M3, 1><<<kShares, 256, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
+  hipError_t e;
+  if (p.many) {
+    a.few = p.few ? kFewRows : 0;
+    if ((e = launch_attend_many(a, D, E4M3, st)) != hipSuccess) return e;
+  } else {
+    a.few = 0x7fffffff;
+  }
+  if (p.few) {
+    attend_few_rows<D, E4M3, 1><<<kShares, 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (!p.few && a.splits == 1) return hipSuccess;
   attend_join<D, 16><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attend_cache_ws_bytes(const CacheArgs& c) {
-  return align256((size_t)(c.n_seqs + 1) * 8) + align256(2 * (size_t)kShares * 16 * 2 * 4) + align256(2 * (size_t)kShares * 16 * c.d * 4);
-}
+size_t attend_cache_ws_bytes(const CacheArgs& c) { return workspace_of(c, plan_of(c)).total; }
 
 hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float* lse, void* ws, hipStream_t st) {
   Args a;
@@ -494,14 +512,17 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.q_t = c.q_t; a.q_h = c.q_h; a.o_t = c.o_t; a.o_h = c.o_h;
   a.Hq = c.Hq; a.g = c.Hq / c.Hkv; a.window = c.window; a.c = c.scale * kLog2e;
   a.by_g = FastDiv((uint32_t)a.g, (uint64_t)c.n_tokens * a.g + 1);
+  const Plan p = plan_of(c);
+  const Workspace w = workspace_of(c, p);
   char* base = (char*)ws;
   a.before = (unsigned long long*)base;
-  base += align256((size_t)(c.n_seqs + 1) * 8);
-  a.part_ml = (float*)base;
-  base += align256(2 * (size_t)kShares * 16 * 2 * 4);
-  a.part_o = (float*)base;
-  if (c.d == 128) return c.e4m3 ? launch<128, true>(a, st) : launch<128, false>(a, st);
-  return c.e4m3 ? launch<64, true>(a, st) : launch<64, false>(a, st);
+  a.part_ml = (float*)(base + w.part_ml);
+  a.part_o = (float*)(base + w.part_o);
+  a.many_ml = (float*)(base + w.many_ml);
+  a.many_o = (float*)(base + w.many_o);
+  a.slots = p.slots; a.splits = p.splits;
+  if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
+  return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }
 
 }  // namespace tsa

@@ -32,20 +32,24 @@ struct Batch {
   }
 };
 
-// Sequence that token t of the packed rows belongs to: the last i with cu_q[i] <= t, by the whole wavefront together, 64 samples
-// of the ascending array per round (one round up to 64 sequences, two up to 4096).  t is the same in all lanes.  Returns n_seqs for
-// a token behind the last sequence, -1 for one in front of the first.
-__device__ __forceinline__ int sequence_of(const Batch& b, int t, int lane) {
-  int lo = 0, n = b.n_seqs + 1;                          // candidates lo .. lo + n - 1: entries of cu_q
+// The last i in 0 .. n_seqs with key(i) <= t, by the whole wavefront together, 64 samples of the ascending keys per round (one round up to
+// 64 sequences, two up to 4096); -1: none.  t is the same in all lanes.
+template <typename F>
+__device__ __forceinline__ int last_up_to(int n_seqs, int t, int lane, F&& key) {
+  int lo = 0, n = n_seqs + 1;                            // candidates lo .. lo + n - 1
   while (n > 0) {
     const int stride = (n + 63) >> 6, i = lo + lane * stride;
-    const bool at_or_before = lane * stride < n && b.cu_q[i] <= t;
-    const int k = __popcll(__builtin_amdgcn_ballot_w64(at_or_before));       // ascending: lanes 0 .. k - 1
-    if (k == 0) return lo - 1;
+    const bool up_to = lane * stride < n && key(i) <= t;
+    const int k = __popcll(__builtin_amdgcn_ballot_w64(up_to));              // ascending: lanes 0 .. k - 1
+    if (k == 0) break;
     lo += (k - 1) * stride + 1;
-    n = min(stride - 1, b.n_seqs + 1 - lo);
+    n = min(stride - 1, n_seqs + 1 - lo);
   }
   return lo - 1;
+}
+// Sequence that token t of the packed rows belongs to: n_seqs for a token behind the last sequence, -1 for one in front of the first.
+__device__ __forceinline__ int sequence_of(const Batch& b, int t, int lane) {
+  return last_up_to(b.n_seqs, t, lane, [&](int i) { return b.cu_q[i]; });
 }
 
 __device__ __forceinline__ float exponent_value(uint32_t byte) { return __uint_as_float(byte << 23); }     // 2^(byte - 127), byte 1 .. 254
