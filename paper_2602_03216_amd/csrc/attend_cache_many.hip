@@ -271,7 +271,99 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a) {
     }
   }
 
+  // ---- the pipelined iteration: a tile that all rows of the workgroup see in full, as they do the one after it.  Same stream of chunks as in
+  // attend.hip: one product and the vector work beside it that does not depend on it, fragments three chunks ahead through a ring of four.
+  //    0 ..  7  S^T(t, half 1)         with  exp of half 0 (sA)
+  //    8 .. 15  O^T += (t, half 0)     with  s c - m and the row max of half 1      [then the rare raise of m]
+  //   16 .. 23  S^T(t + 1, half 0)     with  exp of half 1 (sB)
+  //   24 .. 31  O^T += (t, half 1)     with  s c - m and the row max of (t + 1, half 0)   [wait, barrier, rare raise of m]
+  constexpr int kAhead = 3, kRing = 4, kChunks = 4 * NS, CPB = NS;
+  static_assert(NS == 8 || NS == 4, "the stream is laid out for d = 128 or 64");
+  bf16x8 fr[kRing];
+  auto fetch = [&](int k, int half1, int next0, int v_tile) {
+    const int blk = k / CPB, i = k % CPB;
+    if (blk == 0) fr[k % kRing] = k_frag(half1, i);
+    else if (blk == 2) fr[k % kRing] = k_frag(next0, i);
+    else fr[k % kRing] = v_frag(v_tile, (blk == 3 ? 2 : 0) + i / ND, i % ND);
+  };
+  auto fast_iter = [&]() {
+    float mx = 0.f, ps0 = 0.f, ps1 = 0.f, mxc[1];
+    f32x16 acc;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      const int blk = k / CPB, i = k % CPB;
+      if (i == 0) {                                      // the blocks with exponentials go first (see attend.hip)
+        if (blk == 0 || blk == 2) __builtin_amdgcn_s_setprio(2);
+        else __builtin_amdgcn_s_setprio(0);
+      }
+      if (k + kAhead < kChunks) fetch(k + kAhead, kr[0], kr[1], vc);
+      else fetch(k + kAhead - kChunks, kr[2], kr[3], vn);
+      if constexpr (E4M3) {
+        if (k == 0) load_staged(sk, a.kp, a.ks, r2);
+        if (k == 1) load_staged(sv, a.vp, a.vs, r1);
+        if (k == 3 * CPB) put_k(kr[3], kr[4]);
+        if (k == 3 * CPB + CPB / 2) put_v(vn);
+      } else {
+        if (k < T::CH) load_k_block(r2, kr[3], kr[4], k);
+        else if (k < 2 * T::CH) load_v_block(r1, vn, k - T::CH);
+      }
+      if (blk == 0 || blk == 2) {
+        const f32x16& s_in = blk == 0 ? sA[0] : sB[0];
+        uint32_t (&p_out)[8] = blk == 0 ? pA[0] : pB[0];
+        constexpr int EPS = 16 / NS;
+        if (i == 0) acc = f32x16{0};
+        acc = mfma32(fr[k % kRing], qf[i], acc);
+#pragma unroll
+        for (int e = 0; e < EPS; e += 2) {
+          const int r = EPS * i + e;
+          const float p0 = fast_exp2(s_in[r]), p1 = fast_exp2(s_in[r + 1]);
+          if (r == 0) { ps0 = p0; ps1 = p1; }
+          else { ps0 += p0; ps1 += p1; }
+          p_out[r >> 1] = attend_detail::pack_bf16(p0, p1);
+        }
+        if (i == CPB - 1) {
+          (blk == 0 ? sB[0] : sA[0]) = acc;
+          l[0] += ps0 + ps1;
+        }
+      } else {
+        f32x16& s_in = blk == 1 ? sB[0] : sA[0];
+        const uint32_t (&pb)[8] = blk == 1 ? pA[0] : pB[0];
+        constexpr int EPC = 16 / CPB;
+        o[0][i % ND] = mfma32(fr[k % kRing], attend_detail::p_operand(pb, i / ND), o[0][i % ND]);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) s_in[EPC * i + e] = fmaf(s_in[EPC * i + e], c, -m[0]);
+        if (i == 0) mx = s_in[0];
+#pragma unroll
+        for (int e = 0; e < EPC; e += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s_in[EPC * i + e]), s_in[EPC * i + e + 1]);
+        if (i == CPB - 1) mxc[0] = fmaxf(mx, __shfl_xor(mx, 32));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (k == 2 * CPB - 1) attend_detail::raise_max_rel<ND, 1>(mxc, m, l, o, sB);
+    }
+    wait_loads();
+    lds_barrier();
+    attend_detail::raise_max_rel<ND, 1>(mxc, m, l, o, sA);
+  };
+
+  const float inv_c = 1.0f / c;
   for (int t = t0; t < t1; ++t) {
+    if (full(t, g0) && full(t + 1, g1)) {
+      // (the pipelined iterations hold a half tile as s c - m)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sA[0][r] = fmaf(sA[0][r], c, -m[0]);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) fetch(k, kr[0], kr[1], vc);
+      do {
+        fast_iter();
+        r1 = r2;
+        g0 = g1; g1 = g2;
+        r2 = look_up(t + 3, g2);
+        rotate();
+        ++t;
+      } while (full(t, g0) && full(t + 1, g1));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sA[0][r] = (sA[0][r] + m[0]) * inv_c;
+    }
     load_k(r2, kr[3], kr[4]);
     load_v_seen(r1, t + 1, g1, vn);
     int g3;
