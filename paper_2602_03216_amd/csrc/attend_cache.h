@@ -18,7 +18,6 @@ namespace attend_cache_detail {
 constexpr float kNone = attend_detail::kNegBig;          // running max of a row that has seen no key
 constexpr float kLag = attend_detail::kLazy;             // log2 units that the running max may lag behind
 constexpr int kStep = 128;                               // keys of a step
-constexpr int kShares = 512;                             // workgroups: two per CU
 constexpr int kTile = 64;                                // many rows: keys of a tile
 constexpr int kPartTiles = 8;                            // ... and fewest tiles of a part
 
@@ -37,14 +36,15 @@ struct Args {
   FastDiv by_g;
   // workspace
   unsigned long long* before;    // [n_seqs + 1] steps in front of every sequence
-  float* part_o;                 // [2 kShares][RT][d]
-  float* part_ml;                // [2 kShares][RT][2]
+  float* part_o;                 // [2 shares][rt][d]
+  float* part_ml;                // [2 shares][rt][2]
+  int rt, shares;                // rows of a tile, shares that the steps are cut into
   // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
   int few, splits, slots;
   float* many_o;                 // [slots][Hkv][splits][128][d]
   float* many_ml;                // [slots][Hkv][splits][128][2]
   int split_log2, vheads_per_xcd;
-  FastDiv by_vheads, by_splits;
+  FastDiv by_vheads, by_splits, by_few;
 };
 
 // 64 lanes' 16 bytes to LDS bytes lds .. lds + 1023.  Counted by vmcnt and by nothing that the compiler tracks; no output register.  The wait

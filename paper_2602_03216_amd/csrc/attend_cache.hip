@@ -34,15 +34,14 @@ struct Seq {
   __device__ __forceinline__ unsigned long long units(int Hkv) const { return (unsigned long long)Hkv * tiles * steps; }
 };
 
-template <int RT>
-__device__ __forceinline__ Seq sequence(const Args& a, int i) {
+__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) {
   Seq s;
   s.q0 = a.b.first(i);
   s.q_len = max(a.b.first(i + 1) - s.q0, 0);
   s.kv = a.b.kv(i);
   s.rows = s.q_len * a.g;
   if (s.rows > a.few) s.rows = 0;
-  s.tiles = (s.rows + RT - 1) / RT;
+  s.tiles = (s.rows + rt - 1) / rt;
   s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
   s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
   return s;
@@ -55,6 +54,7 @@ __device__ __forceinline__ uint32_t divide(unsigned long long n, unsigned long l
 template <int D, bool E4M3, int MB>
 struct Shape {
   static constexpr int RT = 16 * MB;                     // rows of a tile
+  static constexpr int kPerCU = MB == 4 ? 1 : 2, kShares = 256 * kPerCU;     // workgroups: what the registers let run at once
   static constexpr int RB = E4M3 ? D : 2 * D;            // bytes of a cached row
   static constexpr int LPR = RB / 16, RPI = 64 / LPR;    // lanes per row, rows of a load into LDS
   static constexpr int NK = RB / 64;                     // 16-byte pieces of a row of K per lane
@@ -78,9 +78,9 @@ struct StepRegs {
 };
 
 template <int D, bool E4M3, int MB>
-__global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
+__global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) {
   using S = Shape<D, E4M3, MB>;
-  constexpr int RT = S::RT, RB = S::RB;
+  constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
   __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
   __shared__ float ml[4][RT][2];
   __shared__ unsigned long long scan[4];
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
   {
     const int per = (n + 255) / 256;
     unsigned long long mine = 0;
-    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += sequence<RT>(a, i).units(Hkv);
+    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += sequence(a, i, RT).units(Hkv);
     unsigned long long upto = mine;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
     unsigned long long at = upto - mine;
     if (blockIdx.x == 0 || (u0 >= at && u0 < upto)) {
       for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
-        const unsigned long long u = sequence<RT>(a, i).units(Hkv);
+        const unsigned long long u = sequence(a, i, RT).units(Hkv);
         if (blockIdx.x == 0) a.before[i] = at;
         if (u0 >= at && u0 < at + u) {
           place[0] = i;
@@ -137,8 +137,8 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
   const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
 
   while (u < end) {
-    Seq q = sequence<RT>(a, seq);
-    while (q.tiles == 0) q = sequence<RT>(a, ++seq);      // (u < total: there is one)
+    Seq q = sequence(a, seq, RT);
+    while (q.tiles == 0) q = sequence(a, ++seq, RT);      // (u < total: there is one)
     const uint32_t ht = divide(in_seq, q.steps), h = ht / q.tiles, tile = ht - h * q.tiles;
     const int s0 = (int)(in_seq - (unsigned long long)ht * q.steps);
     const int s1 = (int)(end - u < (unsigned long long)(q.steps - s0) ? s0 + (int)(end - u) : q.steps);
@@ -363,18 +363,35 @@ __global__ __launch_bounds__(256, 2) void attend_few_rows(Args a) {
   }
 }
 
-// Joins the parts of the rows that no share had whole: one workgroup per token and query head, the parts dealt over its wavefronts.
-// A row tile's first part is the second slot of its share, every later one the first slot of its share.
-template <int D, int RT>
+// Joins the parts of the rows that no share had whole: one workgroup per row, the parts dealt over its wavefronts.  A row tile's first part
+// is the second slot of its share, every later one the first slot of its share.  Rows are counted per sequence where few of the tokens can have
+// parts (BY_SEQUENCE: `few` rows of every sequence and KV head), else per token.
+template <int D, bool BY_SEQUENCE>
 __global__ __launch_bounds__(256) void attend_join(Args a) {
   __shared__ float meet[4][D];
   __shared__ float ml[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int t = blockIdx.x, head = blockIdx.y, h = (int)a.by_g.div(head);
-  const int seq = sequence_of(a.b, t, lane);
-  if (seq < 0 || seq >= a.b.n_seqs) return;
-  const Seq q = sequence<RT>(a, seq);
-  if (t < q.q0 || t >= q.q0 + q.q_len) return;
+  int t, head, h, seq;
+  Seq q;
+  if (BY_SEQUENCE) {
+    seq = blockIdx.y + gridDim.y * blockIdx.z;
+    if (seq >= a.b.n_seqs) return;
+    q = sequence(a, seq, a.rt);
+    h = (int)a.by_few.div(blockIdx.x);
+    const int r = blockIdx.x - h * a.few;
+    if (r >= q.rows) return;
+    const int tok = (int)a.by_g.div(r);
+    t = q.q0 + tok;
+    head = h * a.g + r - tok * a.g;
+  } else {
+    t = blockIdx.x;
+    head = blockIdx.y;
+    h = (int)a.by_g.div(head);
+    seq = sequence_of(a.b, t, lane);
+    if (seq < 0 || seq >= a.b.n_seqs) return;
+    q = sequence(a, seq, a.rt);
+    if (t < q.q0 || t >= q.q0 + q.q_len) return;
+  }
   const int r = (t - q.q0) * a.g + head - h * a.g;
   // parts 0 .. parts - 1: row `first` of the slots, then `next`, `next` + every, ..
   const float *part_o, *part_ml;
@@ -389,14 +406,14 @@ __global__ __launch_bounds__(256) void attend_join(Args a) {
     part_o = a.many_o;
     part_ml = a.many_ml;
   } else {
-    const unsigned long long total = a.before[a.b.n_seqs], share = (total + kShares - 1) / kShares;
-    const int tile = r / RT;
+    const unsigned long long total = a.before[a.b.n_seqs], share = (total + a.shares - 1) / a.shares;
+    const int tile = r / a.rt;
     const unsigned long long u0 = a.before[seq] + ((unsigned long long)h * q.tiles + tile) * q.steps, u1 = u0 + q.steps;
     const int w0 = (int)divide(u0, share), w1 = (int)divide(u1 - 1, share);
     parts = w1 - w0 + 1;
-    first = (2LL * w0 + 1) * RT + r - tile * RT;
-    every = 2 * RT;
-    next = first + RT;
+    first = (2LL * w0 + 1) * a.rt + r - tile * a.rt;
+    every = 2 * a.rt;
+    next = first + a.rt;
     part_o = a.part_o;
     part_ml = a.part_ml;
   }
@@ -443,19 +460,22 @@ __global__ __launch_bounds__(256) void attend_join(Args a) {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Sequences with at most this many rows (new tokens times heads of a group) are dealt by keys, the others by rows.
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 64;
 
-// How a call is cut, from what the host knows: whether any sequence may have many rows, the slots for row tiles, and into how many parts
-// their keys are cut so that 512 workgroups run.
+// How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
+// and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
 struct Plan {
   bool few, many;
-  int slots, splits;
+  int mb, shares, slots, splits;
 };
 Plan plan_of(const CacheArgs& c) {
   const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
   Plan p;
   p.many = (long long)most * g > kFewRows;
   p.few = !p.many || c.n_seqs > 1;
+  const int rows = p.many ? g : most * g;                // (beside prompts: single tokens, most likely)
+  p.mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.shares = p.mb == 4 ? 256 : 512;
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
   const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
   const long long keys = (long long)c.max_pages << c.page_log2, most_parts = keys / (kTile * kPartTiles);
@@ -472,11 +492,11 @@ Workspace workspace_of(const CacheArgs& c, const Plan& p) {
   Workspace w;
   size_t at = align256((size_t)(c.n_seqs + 1) * 8);
   auto take = [&](size_t n) { const size_t x = at; at += align256(n); return x; };
-  w.part_ml = take(2 * (size_t)kShares * 16 * 2 * 4);
-  w.part_o = take(2 * (size_t)kShares * 16 * c.d * 4);
-  const size_t rows = p.many && p.splits > 1 ? (size_t)p.slots * c.Hkv * p.splits * kManyRows : 0;
-  w.many_ml = take(rows * 2 * 4);
-  w.many_o = take(rows * c.d * 4);
+  const size_t few = 2 * (size_t)p.shares * 16 * p.mb, many = p.many && p.splits > 1 ? (size_t)p.slots * c.Hkv * p.splits * kManyRows : 0;
+  w.part_ml = take(few * 2 * 4);
+  w.part_o = take(few * c.d * 4);
+  w.many_ml = take(many * 2 * 4);
+  w.many_o = take(many * c.d * 4);
   w.total = at;
   return w;
 }
@@ -484,18 +504,23 @@ Workspace workspace_of(const CacheArgs& c, const Plan& p) {
 template <int D, bool E4M3>
 hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
   hipError_t e;
-  if (p.many) {
-    a.few = p.few ? kFewRows : 0;
-    if ((e = launch_attend_many(a, D, E4M3, st)) != hipSuccess) return e;
-  } else {
-    a.few = 0x7fffffff;
-  }
+  a.few = p.many ? (p.few ? kFewRows : 0) : 0x7fffffff;
+  if (p.many && (e = launch_attend_many(a, D, E4M3, st)) != hipSuccess) return e;
   if (p.few) {
-    attend_few_rows<D, E4M3, 1><<<kShares, 256, 0, st>>>(a);
+    if (p.mb == 1) attend_few_rows<D, E4M3, 1><<<p.shares, 256, 0, st>>>(a);
+    else if (p.mb == 2) attend_few_rows<D, E4M3, 2><<<p.shares, 256, 0, st>>>(a);
+    else attend_few_rows<D, E4M3, 4><<<p.shares, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (!p.few && a.splits == 1) return hipSuccess;
-  attend_join<D, 16><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+  if (!p.few && p.splits == 1) return hipSuccess;
+  // rows that can have parts: all, or those of sequences with few
+  if (p.many && p.splits == 1 && (long long)a.b.n_seqs * kFewRows < (long long)a.b.n_tokens * a.g) {
+    a.by_few = FastDiv((uint32_t)a.few, (uint64_t)a.b.Hkv * a.few);
+    const int y = a.b.n_seqs < 32768 ? a.b.n_seqs : 32768;
+    attend_join<D, true><<<dim3(a.b.Hkv * a.few, y, (a.b.n_seqs + y - 1) / y), 256, 0, st>>>(a);
+  } else {
+    attend_join<D, false><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -520,7 +545,7 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.slots = p.slots; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.shares = p.shares; a.slots = p.slots; a.splits = p.splits;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }
