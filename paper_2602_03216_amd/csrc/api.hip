@@ -694,7 +694,7 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
   int rc;
   if ((rc = check_cache_desc(desc, &c))) return rc;
   if (L < 0 || L >= (1 << 30)) return fail(TSA_ERR_ARG, "L (%d) must lie in [0, 2^30)", L);
-  if ((long long)c.n_seqs * c.Hkv * ((L + 127LL) / 128) > 0x7fffffffLL) return fail(TSA_ERR_UNSUPPORTED, "grid too large");
+  if ((long long)c.n_seqs * c.Hkv * ((L + 15LL) / 16) > 0x7fffffffLL) return fail(TSA_ERR_UNSUPPORTED, "grid too large");
   if (L == 0) return TSA_OK;
   if ((rc = check_ptr(K, "K")) || (rc = check_ptr(V, "V"))) return rc;
   if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
