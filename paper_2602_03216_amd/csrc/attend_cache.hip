@@ -88,31 +88,36 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
   const int n = a.b.n_seqs, Hkv = a.b.Hkv;
 
-  // ---- the share: thread t counts sequences t * per .. of the batch
+  // ---- the share: thread t counts sequences t * per .. of the batch.  Up to 64 sequences every wavefront does it for itself, a sequence per lane.
   unsigned long long total, share;
   {
-    const int per = (n + 255) / 256;
+    const bool alone = n <= 64;
+    const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
     unsigned long long mine = 0;
-    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += sequence(a, i, RT).units(Hkv);
+    for (int i = i0; i < i1; ++i) mine += sequence(a, i, RT).units(Hkv);
     unsigned long long upto = mine;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
       const unsigned long long o = __shfl_up(upto, m);
       if (lane >= m) upto += o;
     }
-    if (lane == 63) scan[wave] = upto;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) upto += scan[w];
-      total += scan[w];
+    if (alone) {
+      total = __shfl(upto, 63);
+    } else {
+      if (lane == 63) scan[wave] = upto;
+      __syncthreads();
+      total = 0;
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) upto += scan[w];
+        total += scan[w];
+      }
     }
     share = (total + kShares - 1) / kShares;
     const unsigned long long u0 = blockIdx.x * share;
     unsigned long long at = upto - mine;
     if (blockIdx.x == 0 || (u0 >= at && u0 < upto)) {
-      for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
-        const unsigned long long u = sequence(a, i, RT).units(Hkv);
+      for (int i = i0; i < i1; ++i) {
+        const unsigned long long u = alone ? mine : sequence(a, i, RT).units(Hkv);
         if (blockIdx.x == 0) a.before[i] = at;
         if (u0 >= at && u0 < at + u) {
           place[0] = i;
@@ -363,14 +368,17 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
   }
 }
 
-// Joins the parts of the rows that no share had whole: one workgroup per row, the parts dealt over its wavefronts.  A row tile's first part
+// Joins the parts of the rows that no share had whole: one workgroup per row.  A row tile's first part
 // is the second slot of its share, every later one the first slot of its share.  Rows are counted per sequence where few of the tokens can have
 // parts (BY_SEQUENCE: `few` rows of every sequence and KV head), else per token.
+constexpr int kMostParts = 512;                          // shares, or parts of a row tile's keys: no row has more
 template <int D, bool BY_SEQUENCE>
 __global__ __launch_bounds__(256) void attend_join(Args a) {
-  __shared__ float meet[4][D];
+  constexpr int LPR = D / 4, G = 256 / LPR, kBatch = 4;   // lanes of a row, four values each; groups of lanes that take every G-th part
+  __shared__ float weight[kMostParts];
+  __shared__ float meet[G][D];
   __shared__ float ml[4][2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int t, head, h, seq;
   Seq q;
   if (BY_SEQUENCE) {
@@ -418,43 +426,59 @@ __global__ __launch_bounds__(256) void attend_join(Args a) {
     part_ml = a.part_ml;
   }
   if (parts == 1) return;
-  constexpr int N = D / 64;
-  float m = kNone, l = 0.f, o[N] = {};
-  for (int w = wave; w < parts; w += 4) {
-    const long long slot = w == 0 ? first : next + (long long)(w - 1) * every;
-    const float mp = part_ml[2 * slot], lp = part_ml[2 * slot + 1];
-    float v[N];
+  const auto place = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * every; };
+  const int grp = tid / LPR, col = 4 * (tid % LPR);
+  f32x4 v[kBatch];
+  const auto rows_from = [&](int w0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = part_o[slot * D + N * lane + i];
-    const float mn = fmaxf(m, mp), x = fast_exp2(m - mn), y = fast_exp2(mp - mn);
+    for (int i = 0; i < kBatch; ++i) v[i] = w0 + i * G < parts ? *(const f32x4*)(part_o + place(w0 + i * G) * D + col) : f32x4{0, 0, 0, 0};
+  };
+  rows_from(grp);
+  // all parts' running maxima and sums, so that rows wait for nothing
+  float m = kNone, l = 0.f;
+  for (int w = tid; w < parts; w += 256) {
+    const float mp = part_ml[2 * place(w)], lp = part_ml[2 * place(w) + 1], mn = fmaxf(m, mp);
+    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
     m = mn;
-    l = l * x + lp * y;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * x + v[i] * y;
+    weight[w] = mp;
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) meet[wave][N * lane + i] = o[i];
+  for (int x = 1; x < 64; x <<= 1) {
+    const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
+    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+    m = mn;
+  }
   if (lane == 0) {
     ml[wave][0] = m;
     ml[wave][1] = l;
   }
   __syncthreads();
-  if (threadIdx.x >= D / 2) return;
   const float mt = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
-  float lt = 0.f, v0 = 0.f, v1 = 0.f;
+  float lt = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float x = fast_exp2(ml[w][0] - mt);
-    lt += ml[w][1] * x;
-    v0 += meet[w][2 * threadIdx.x] * x;
-    v1 += meet[w][2 * threadIdx.x + 1] * x;
+  for (int w = 0; w < 4; ++w) lt += ml[w][1] * fast_exp2(ml[w][0] - mt);
+  f32x4 o = {0, 0, 0, 0};
+  for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (w0 + i * G < parts) o += v[i] * fast_exp2(weight[w0 + i * G] - mt);
+    rows_from(w0 + kBatch * G);
+  }
+  *(f32x4*)(&meet[grp][col]) = o;
+  __syncthreads();
+  if (tid >= D / 2) return;
+  float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < G; ++w) {
+    v0 += meet[w][2 * tid];
+    v1 += meet[w][2 * tid + 1];
   }
   const float inv = lt > 0.f ? 1.0f / lt : 0.f;
   bf16x2 out;
   out[0] = (__bf16)(v0 * inv);
   out[1] = (__bf16)(v1 * inv);
-  *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + 2 * threadIdx.x) = out;
-  if (a.lse && threadIdx.x == 0) a.lse[(long long)t * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+  *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + 2 * tid) = out;
+  if (a.lse && tid == 0) a.lse[(long long)t * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -481,7 +505,7 @@ Plan plan_of(const CacheArgs& c) {
   const long long keys = (long long)c.max_pages << c.page_log2, most_parts = keys / (kTile * kPartTiles);
   long long s = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
   if (s > most_parts) s = most_parts;
-  p.splits = s < 1 ? 1 : (int)s;
+  p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
   return p;
 }
 
