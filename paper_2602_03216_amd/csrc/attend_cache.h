@@ -21,6 +21,11 @@ constexpr int kStep = 128;                               // keys of a step
 constexpr int kTile = 64;                                // many rows: keys of a tile
 constexpr int kPartTiles = 8;                            // ... and fewest tiles of a part
 
+// A row tile that does not end in the share it begins in (parts: 0 = there is none), parts of it, its rows.
+struct Cut {
+  int parts, q0, head, row0, rows;
+};
+
 struct Args {
   Batch b;
   const __bf16* Q;
@@ -35,16 +40,16 @@ struct Args {
   float c;                       // scale * log2(e)
   FastDiv by_g;
   // workspace
-  unsigned long long* before;    // [n_seqs + 1] steps in front of every sequence
+  Cut* cut;                      // [shares]
   float* part_o;                 // [2 shares][rt][d]
   float* part_ml;                // [2 shares][rt][2]
-  int rt, shares;                // rows of a tile, shares that the steps are cut into
+  int rt;                        // rows of a tile
   // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
   int few, splits, slots;
   float* many_o;                 // [slots][Hkv][splits][128][d]
   float* many_ml;                // [slots][Hkv][splits][128][2]
   int split_log2, vheads_per_xcd;
-  FastDiv by_vheads, by_splits, by_few;
+  FastDiv by_vheads, by_splits;
 };
 
 // 64 lanes' 16 bytes to LDS bytes lds .. lds + 1023.  Counted by vmcnt and by nothing that the compiler tracks; no output register.  The wait

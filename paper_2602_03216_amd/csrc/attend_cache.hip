@@ -51,10 +51,15 @@ __device__ __forceinline__ uint32_t divide(unsigned long long n, unsigned long l
   return (n | d) >> 32 ? (uint32_t)(n / d) : (uint32_t)n / (uint32_t)d;
 }
 
+// Shares per CU, all of which run at once.  What they have in flight together is what the memory rate comes from: the rows of d = 64 in 8 bits
+// are short and take four (300 sequences x 1000 keys, 8 KV heads: 97 -> 81 us, 6 x 131072 158 -> 151); with longer rows two have enough in
+// flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 195 us with two, 207 with three; bf16, d = 64: 189 with two, 195 with four).
+constexpr int per_cu(int d, bool e4m3, int mb) { return mb == 4 && d == 128 ? 1 : mb == 1 && d == 64 && e4m3 ? 4 : 2; }
+
 template <int D, bool E4M3, int MB>
 struct Shape {
   static constexpr int RT = 16 * MB;                     // rows of a tile
-  static constexpr int kPerCU = MB == 4 ? 1 : 2, kShares = 256 * kPerCU;     // workgroups: what the registers let run at once
+  static constexpr int kPerCU = per_cu(D, E4M3, MB), kShares = 256 * kPerCU;
   static constexpr int RB = E4M3 ? D : 2 * D;            // bytes of a cached row
   static constexpr int LPR = RB / 16, RPI = 64 / LPR;    // lanes per row, rows of a load into LDS
   static constexpr int NK = RB / 64;                     // 16-byte pieces of a row of K per lane
@@ -78,7 +83,7 @@ struct StepRegs {
 };
 
 template <int D, bool E4M3, int MB>
-__global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) {
+__global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args a) {
   using S = Shape<D, E4M3, MB>;
   constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
   __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
@@ -88,11 +93,10 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
   const int n = a.b.n_seqs, Hkv = a.b.Hkv;
 
-  // ---- the share: thread t counts sequences t * per .. of the batch.  Up to 64 sequences every wavefront does it for itself, a sequence per lane.
+  // ---- the share: thread t counts sequences t * per .. of the batch
   unsigned long long total, share;
   {
-    const bool alone = n <= 64;
-    const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
+    const int per = (n + 255) / 256, i0 = tid * per, i1 = min(n, i0 + per);
     unsigned long long mine = 0;
     for (int i = i0; i < i1; ++i) mine += sequence(a, i, RT).units(Hkv);
     unsigned long long upto = mine;
@@ -101,32 +105,26 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
       const unsigned long long o = __shfl_up(upto, m);
       if (lane >= m) upto += o;
     }
-    if (alone) {
-      total = __shfl(upto, 63);
-    } else {
-      if (lane == 63) scan[wave] = upto;
-      __syncthreads();
-      total = 0;
-      for (int w = 0; w < 4; ++w) {
-        if (w < wave) upto += scan[w];
-        total += scan[w];
-      }
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) upto += scan[w];
+      total += scan[w];
     }
     share = (total + kShares - 1) / kShares;
     const unsigned long long u0 = blockIdx.x * share;
     unsigned long long at = upto - mine;
-    if (blockIdx.x == 0 || (u0 >= at && u0 < upto)) {
+    if (u0 >= at && u0 < upto)
       for (int i = i0; i < i1; ++i) {
-        const unsigned long long u = alone ? mine : sequence(a, i, RT).units(Hkv);
-        if (blockIdx.x == 0) a.before[i] = at;
+        const unsigned long long u = sequence(a, i, RT).units(Hkv);
         if (u0 >= at && u0 < at + u) {
           place[0] = i;
           place[1] = u0 - at;
         }
         at += u;
       }
-      if (blockIdx.x == 0 && tid == 0) a.before[n] = total;
-    }
+    if (tid == 0) a.cut[blockIdx.x].parts = 0;
     if (u0 >= total) return;
     __syncthreads();
   }
@@ -327,6 +325,10 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
     }
     __syncthreads();
     const bool whole = s0 == 0 && s1 == q.steps;
+    if (s0 == 0 && s1 < q.steps && tid == 0) {             // the shares that follow go on with it
+      const int more = (int)(((unsigned long long)(q.steps - s1) + share - 1) / share);
+      a.cut[blockIdx.x] = Cut{1 + more, q.q0, (int)h, row0, min(RT, q.rows - row0)};
+    }
     const long long slot = 2LL * blockIdx.x + (s0 == 0 ? 1 : 0);
     for (int task = tid; task < RT * (D / 8); task += 256) {
       const int r = task / (D / 8), col = 8 * (task % (D / 8));
@@ -368,117 +370,145 @@ __global__ __launch_bounds__(256, MB == 4 ? 1 : 2) void attend_few_rows(Args a) 
   }
 }
 
-// Joins the parts of the rows that no share had whole: one workgroup per row.  A row tile's first part
-// is the second slot of its share, every later one the first slot of its share.  Rows are counted per sequence where few of the tokens can have
-// parts (BY_SEQUENCE: `few` rows of every sequence and KV head), else per token.
-constexpr int kMostParts = 512;                          // shares, or parts of a row tile's keys: no row has more
-template <int D, bool BY_SEQUENCE>
-__global__ __launch_bounds__(256) void attend_join(Args a) {
-  constexpr int LPR = D / 4, G = 256 / LPR, kBatch = 4;   // lanes of a row, four values each; groups of lanes that take every G-th part
-  __shared__ float weight[kMostParts];
-  __shared__ float meet[G][D];
+constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
+
+// The sum of the parts of `R` rows: wavefront r finds row r's largest max and its sum, then groups of lanes take every G-th part of all of them.
+//   parts of row r: slot_of(part) + r of the arrays part_o [..][D] and part_ml [..][2];  out(r, col, v0, v1) gets two columns of a finished
+//   row, lse(r, value) its log-sum-exp.  rows: how many of the R there are.
+template <int D, int R, typename P, typename O, typename L>
+__device__ __forceinline__ void join_rows(const float* part_o, const float* part_ml, int parts, int rows, P&& slot_of, O&& out, L&& lse) {
+  constexpr int LPR = D / 4, G = 256 / LPR, kBatch = 8 / R;
+  static_assert(R == 1 || R == 4, "wavefronts are dealt over rows, or all take one");
+  __shared__ float weight[R][kMostParts];
+  __shared__ float meet[G][R][D];
   __shared__ float ml[4][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int t, head, h, seq;
-  Seq q;
-  if (BY_SEQUENCE) {
-    seq = blockIdx.y + gridDim.y * blockIdx.z;
-    if (seq >= a.b.n_seqs) return;
-    q = sequence(a, seq, a.rt);
-    h = (int)a.by_few.div(blockIdx.x);
-    const int r = blockIdx.x - h * a.few;
-    if (r >= q.rows) return;
-    const int tok = (int)a.by_g.div(r);
-    t = q.q0 + tok;
-    head = h * a.g + r - tok * a.g;
-  } else {
-    t = blockIdx.x;
-    head = blockIdx.y;
-    h = (int)a.by_g.div(head);
-    seq = sequence_of(a.b, t, lane);
-    if (seq < 0 || seq >= a.b.n_seqs) return;
-    q = sequence(a, seq, a.rt);
-    if (t < q.q0 || t >= q.q0 + q.q_len) return;
-  }
-  const int r = (t - q.q0) * a.g + head - h * a.g;
-  // parts 0 .. parts - 1: row `first` of the slots, then `next`, `next` + every, ..
-  const float *part_o, *part_ml;
-  long long first, next;
-  int parts, every;
-  if (q.rows == 0) {                                     // many rows
-    const ManyTile x = many_tile(a, seq, r / kManyRows);
-    parts = x.parts;
-    first = (((long long)first_slot(a, seq) + r / kManyRows) * a.b.Hkv + h) * a.splits * kManyRows + r % kManyRows;
-    every = kManyRows;
-    next = first + every;
-    part_o = a.many_o;
-    part_ml = a.many_ml;
-  } else {
-    const unsigned long long total = a.before[a.b.n_seqs], share = (total + a.shares - 1) / a.shares;
-    const int tile = r / a.rt;
-    const unsigned long long u0 = a.before[seq] + ((unsigned long long)h * q.tiles + tile) * q.steps, u1 = u0 + q.steps;
-    const int w0 = (int)divide(u0, share), w1 = (int)divide(u1 - 1, share);
-    parts = w1 - w0 + 1;
-    first = (2LL * w0 + 1) * a.rt + r - tile * a.rt;
-    every = 2 * a.rt;
-    next = first + a.rt;
-    part_o = a.part_o;
-    part_ml = a.part_ml;
-  }
-  if (parts == 1) return;
-  const auto place = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * every; };
-  const int grp = tid / LPR, col = 4 * (tid % LPR);
-  f32x4 v[kBatch];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
+  f32x4 v[kBatch][R];
   const auto rows_from = [&](int w0) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) v[i] = w0 + i * G < parts ? *(const f32x4*)(part_o + place(w0 + i * G) * D + col) : f32x4{0, 0, 0, 0};
-  };
-  rows_from(grp);
-  // all parts' running maxima and sums, so that rows wait for nothing
-  float m = kNone, l = 0.f;
-  for (int w = tid; w < parts; w += 256) {
-    const float mp = part_ml[2 * place(w)], lp = part_ml[2 * place(w) + 1], mn = fmaxf(m, mp);
-    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
-    m = mn;
-    weight[w] = mp;
-  }
+    for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) {
-    const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
-    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
-    m = mn;
-  }
-  if (lane == 0) {
-    ml[wave][0] = m;
-    ml[wave][1] = l;
+      for (int r = 0; r < R; ++r)
+        v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
+  };
+  rows_from(grp);                                        // (the rows wait for nothing)
+  {
+    const int r = R == 1 ? 0 : wave, from = R == 1 ? tid : lane, step = R == 1 ? 256 : 64;
+    float m = kNone, l = 0.f;
+    if (r < rows)
+      for (int w = from; w < parts; w += step) {
+        const long long slot = slot_of(w) + r;
+        const float mp = part_ml[2 * slot], lp = part_ml[2 * slot + 1], mn = fmaxf(m, mp);
+        l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+        m = mn;
+        weight[r][w] = mp;
+      }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
+      l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+      m = mn;
+    }
+    if (lane == 0) {
+      ml[wave][0] = m;
+      ml[wave][1] = l;
+    }
   }
   __syncthreads();
-  const float mt = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
-  float lt = 0.f;
+  float mt[R], lt[R];
+  if (R == 1) {
+    mt[0] = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+    lt[0] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) lt += ml[w][1] * fast_exp2(ml[w][0] - mt);
-  f32x4 o = {0, 0, 0, 0};
+    for (int w = 0; w < 4; ++w) lt[0] += ml[w][1] * fast_exp2(ml[w][0] - mt[0]);
+  } else {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mt[r] = ml[r][0];
+      lt[r] = ml[r][1];
+    }
+  }
+  f32x4 o[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
   for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i)
-      if (w0 + i * G < parts) o += v[i] * fast_exp2(weight[w0 + i * G] - mt);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - mt[r]);
     rows_from(w0 + kBatch * G);
   }
-  *(f32x4*)(&meet[grp][col]) = o;
-  __syncthreads();
-  if (tid >= D / 2) return;
-  float v0 = 0.f, v1 = 0.f;
 #pragma unroll
-  for (int w = 0; w < G; ++w) {
-    v0 += meet[w][2 * tid];
-    v1 += meet[w][2 * tid + 1];
+  for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
+  __syncthreads();
+  for (int task = tid; task < R * D / 2; task += 256) {
+    const int r = task / (D / 2), c = 2 * (task % (D / 2));
+    if (r >= rows) continue;
+    float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      v0 += meet[g][r][c];
+      v1 += meet[g][r][c + 1];
+    }
+    float ls = lt[0], ms = mt[0];
+#pragma unroll
+    for (int k = 1; k < R; ++k)
+      if (r == k) { ls = lt[k]; ms = mt[k]; }
+    const float inv = ls > 0.f ? 1.0f / ls : 0.f;
+    out(r, c, v0 * inv, v1 * inv);
+    if (c == 0) lse(r, ls > 0.f ? (ms + log2f(ls)) * kLn2 : -INFINITY);
   }
-  const float inv = lt > 0.f ? 1.0f / lt : 0.f;
-  bf16x2 out;
-  out[0] = (__bf16)(v0 * inv);
-  out[1] = (__bf16)(v1 * inv);
-  *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + 2 * tid) = out;
-  if (a.lse && tid == 0) a.lse[(long long)t * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+}
+
+// Row tiles that a share's end cuts: the workgroup of the share that has a tile's first part, and a group of four of its rows.  The first part is
+// the second slot of its share, every later one the first slot of its share.
+template <int D>
+__global__ __launch_bounds__(256) void join_few_rows(Args a) {
+  const Cut c = a.cut[blockIdx.x];
+  const int r0 = 4 * blockIdx.y;
+  if (c.parts == 0 || r0 >= c.rows) return;
+  const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
+  const auto where = [&](int r, int& tok, int& head) {
+    const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row);
+    tok = c.q0 + k;
+    head = c.head * a.g + row - k * a.g;
+  };
+  join_rows<D, 4>(a.part_o, a.part_ml, c.parts, c.rows - r0, [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; },
+                  [&](int r, int col, float v0, float v1) {
+                    int tok, head;
+                    where(r, tok, head);
+                    bf16x2 v;
+                    v[0] = (__bf16)v0;
+                    v[1] = (__bf16)v1;
+                    *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + col) = v;
+                  },
+                  [&](int r, float v) {
+                    int tok, head;
+                    where(r, tok, head);
+                    if (a.lse) a.lse[(long long)tok * a.Hq + head] = v;
+                  });
+}
+
+// Rows whose keys are cut into parts (many rows): one workgroup per token and query head.
+template <int D>
+__global__ __launch_bounds__(256) void join_many_rows(Args a) {
+  const int t = blockIdx.x, head = blockIdx.y, h = (int)a.by_g.div(head);
+  const int seq = sequence_of(a.b, t, threadIdx.x & 63);
+  if (seq < 0 || seq >= a.b.n_seqs) return;
+  const int q0 = a.b.first(seq), r = (t - q0) * a.g + head - h * a.g;
+  if (t < q0 || t >= a.b.first(seq + 1)) return;
+  const ManyTile x = many_tile(a, seq, r / kManyRows);
+  if (!x.there || x.parts == 1) return;
+  const long long first = (((long long)first_slot(a, seq) + r / kManyRows) * a.b.Hkv + h) * a.splits * kManyRows + r % kManyRows;
+  join_rows<D, 1>(a.many_o, a.many_ml, x.parts, 1, [&](int w) -> long long { return first + (long long)w * kManyRows; },
+                  [&](int, int col, float v0, float v1) {
+                    bf16x2 v;
+                    v[0] = (__bf16)v0;
+                    v[1] = (__bf16)v1;
+                    *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + col) = v;
+                  },
+                  [&](int, float v) { if (a.lse) a.lse[(long long)t * a.Hq + head] = v; });
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -498,11 +528,17 @@ Plan plan_of(const CacheArgs& c) {
   p.many = (long long)most * g > kFewRows;
   p.few = !p.many || c.n_seqs > 1;
   const int rows = p.many ? g : most * g;                // (beside prompts: single tokens, most likely)
-  p.mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.shares = p.mb == 4 ? 256 : 512;
+  // Rows of a tile.  Larger tiles read K and V fewer times, smaller ones start and end sooner and are more of them.  28 / 4 heads, us with tiles of
+  // 16 / 32 / 64 rows: 32 sequences x 8000 keys, 3 new tokens (21 rows) bf16 160 / 109 / 114, 8 bits 87 / 60 / 96; 8 new tokens (56 rows) 298 / 166 / 122
+  // and 155 / 99 / 103; 200 x 500, 56 rows, 131 / 84 / 76 and 83 / 68 / 75; 2 x 300, 56 rows, 11.5 / 13.3 / 17.0 and 11.1 / 13.3 / 16.8; 1 x 2000 15.1 / 16.7 / 19.9.
+  // So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
+  const long long cap = (long long)c.max_pages << c.page_log2, seen = c.window && c.window + (long long)most < cap ? c.window + (long long)most : cap;
+  const bool small = (long long)c.n_seqs * c.Hkv * ((seen + kStep - 1) / kStep) <= 512;
+  p.mb = rows <= 16 || small ? 1 : rows <= 32 || c.e4m3 ? 2 : 4;
+  p.shares = 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
   const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
-  const long long keys = (long long)c.max_pages << c.page_log2, most_parts = keys / (kTile * kPartTiles);
+  const long long most_parts = cap / (kTile * kPartTiles);
   long long s = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
   if (s > most_parts) s = most_parts;
   p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
@@ -514,7 +550,7 @@ struct Workspace {
 };
 Workspace workspace_of(const CacheArgs& c, const Plan& p) {
   Workspace w;
-  size_t at = align256((size_t)(c.n_seqs + 1) * 8);
+  size_t at = align256((size_t)p.shares * sizeof(Cut));
   auto take = [&](size_t n) { const size_t x = at; at += align256(n); return x; };
   const size_t few = 2 * (size_t)p.shares * 16 * p.mb, many = p.many && p.splits > 1 ? (size_t)p.slots * c.Hkv * p.splits * kManyRows : 0;
   w.part_ml = take(few * 2 * 4);
@@ -535,17 +571,14 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
     else if (p.mb == 2) attend_few_rows<D, E4M3, 2><<<p.shares, 256, 0, st>>>(a);
     else attend_few_rows<D, E4M3, 4><<<p.shares, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    join_few_rows<D><<<dim3(p.shares, 4 * p.mb), 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (!p.few && p.splits == 1) return hipSuccess;
-  // rows that can have parts: all, or those of sequences with few
-  if (p.many && p.splits == 1 && (long long)a.b.n_seqs * kFewRows < (long long)a.b.n_tokens * a.g) {
-    a.by_few = FastDiv((uint32_t)a.few, (uint64_t)a.b.Hkv * a.few);
-    const int y = a.b.n_seqs < 32768 ? a.b.n_seqs : 32768;
-    attend_join<D, true><<<dim3(a.b.Hkv * a.few, y, (a.b.n_seqs + y - 1) / y), 256, 0, st>>>(a);
-  } else {
-    attend_join<D, false><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+  if (p.many && p.splits > 1) {
+    join_many_rows<D><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace
@@ -564,12 +597,12 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   const Plan p = plan_of(c);
   const Workspace w = workspace_of(c, p);
   char* base = (char*)ws;
-  a.before = (unsigned long long*)base;
+  a.cut = (Cut*)base;
   a.part_ml = (float*)(base + w.part_ml);
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.rt = 16 * p.mb; a.shares = p.shares; a.slots = p.slots; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.slots = p.slots; a.splits = p.splits;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }
