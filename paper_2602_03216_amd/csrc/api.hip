@@ -717,7 +717,9 @@ int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pa
   if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(O, "O")) || (rc = check_ints(cu_q, "cu_q"))) return rc;
   if (lse && ((uintptr_t)lse & 3u)) return fail(TSA_ERR_ARG, "lse is not 4-byte aligned");
   if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
-  if ((rc = check_ws(ws, ws_bytes, tsa::attend_cache_ws_bytes(c)))) return rc;
+  const size_t need = tsa::attend_cache_ws_bytes(c);
+  if (need == 0) return fail(TSA_ERR_UNSUPPORTED, "n_seqs * Hkv * max_pages * page_size is too large: keys are counted in 2^32 steps of 128");
+  if ((rc = check_ws(ws, ws_bytes, need))) return rc;
   c.cu_q = cu_q;
   return hip_status(tsa::launch_attend_cache(c, Q, O, lse, ws, (hipStream_t)stream), "tsa_attend_cache");
 }

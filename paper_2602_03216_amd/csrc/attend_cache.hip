@@ -31,7 +31,9 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __
 // What a sequence asks for.
 struct Seq {
   int q0, q_len, kv, rows, tiles, first, steps;          // first: its first key that any query sees, rounded down to 16
-  __device__ __forceinline__ unsigned long long units(int Hkv) const { return (unsigned long long)Hkv * tiles * steps; }
+  // steps of all its row tiles, each counted as a multiple of `of`
+  __device__ __forceinline__ uint32_t units(int Hkv, int of) const { return (uint32_t)(Hkv * tiles) * span(of); }
+  __device__ __forceinline__ uint32_t span(int of) const { return of == 1 ? steps : (uint32_t)((steps + of - 1) / of) * of; }
 };
 
 __device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) {
@@ -45,10 +47,6 @@ __device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) {
   s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
   s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
   return s;
-}
-
-__device__ __forceinline__ uint32_t divide(unsigned long long n, unsigned long long d) {       // (quotients fit)
-  return (n | d) >> 32 ? (uint32_t)(n / d) : (uint32_t)n / (uint32_t)d;
 }
 
 // Shares per CU, all of which run at once.  What they have in flight together is what the memory rate comes from: the rows of d = 64 in 8 bits
@@ -88,23 +86,61 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
   constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
   __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
   __shared__ float ml[4][RT][2];
-  __shared__ unsigned long long scan[4];
-  __shared__ unsigned long long place[2];
+  __shared__ uint32_t scan[4], place[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
   const int n = a.b.n_seqs, Hkv = a.b.Hkv;
 
-  // ---- the share: thread t counts sequences t * per .. of the batch
-  unsigned long long total, share;
-  {
-    const int per = (n + 255) / 256, i0 = tid * per, i1 = min(n, i0 + per);
-    unsigned long long mine = 0;
-    for (int i = i0; i < i1; ++i) mine += sequence(a, i, RT).units(Hkv);
-    unsigned long long upto = mine;
+  // ---- the share: thread t counts sequences t * per .. of the batch.  Where a few steps more than an equal share let no share go over the end of
+  // a row tile, the tiles are counted as multiples of such a share: another tile in a share costs a meeting of the wavefronts and a start, which is
+  // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 EEE).
+  // (Up to 64 sequences every wavefront does it for itself, a sequence per lane, without a barrier.)
+  const bool alone = n <= 64;
+  const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
+  const Seq own = sequence(a, min(i0, n - 1), RT);
+  const auto over_mine = [&](auto&& f) {
+    for (int i = i0; i < i1; ++i) f(i, per == 1 ? own : sequence(a, i, RT));
+  };
+  const auto sum_up = [&](uint32_t x) -> uint32_t {
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const unsigned long long o = __shfl_up(upto, m);
-      if (lane >= m) upto += o;
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    if (alone) return x;
+    __syncthreads();
+    if (lane == 0) scan[wave] = x;
+    __syncthreads();
+    return scan[0] + scan[1] + scan[2] + scan[3];
+  };
+  uint32_t mine = 0;
+  over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
+  uint32_t total = sum_up(mine), share = (total + kShares - 1) / kShares;
+  int of = 1;
+  if (share > 1) {
+    for (int k = 0; k < 4 && of == 1; ++k) {
+      uint32_t parts = 0;                                // shares that whole ones of share + k steps make
+      over_mine([&](int, const Seq& q) { parts += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k - 1) / (share + k)); });
+      if (sum_up(parts) <= (uint32_t)kShares) of = (int)share + k;
     }
+    if (of > 1) {
+      share = of;
+      mine = 0;
+      over_mine([&](int, const Seq& q) { mine += q.units(Hkv, of); });
+    }
+  }
+  if (tid == 0) a.cut[blockIdx.x].parts = 0;
+  uint32_t upto = mine;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t o = __shfl_up(upto, m);
+    if (lane >= m) upto += o;
+  }
+  uint32_t u = blockIdx.x * share, in_seq;
+  int seq;
+  if (alone) {
+    total = __shfl(upto, 63);
+    if (u >= total) return;
+    seq = __ffsll((long long)__builtin_amdgcn_ballot_w64(u < upto)) - 1;
+    in_seq = u - __builtin_amdgcn_readlane(upto - mine, seq);
+  } else {
+    __syncthreads();
     if (lane == 63) scan[wave] = upto;
     __syncthreads();
     total = 0;
@@ -112,26 +148,22 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
       if (w < wave) upto += scan[w];
       total += scan[w];
     }
-    share = (total + kShares - 1) / kShares;
-    const unsigned long long u0 = blockIdx.x * share;
-    unsigned long long at = upto - mine;
-    if (u0 >= at && u0 < upto)
-      for (int i = i0; i < i1; ++i) {
-        const unsigned long long u = sequence(a, i, RT).units(Hkv);
-        if (u0 >= at && u0 < at + u) {
+    if (u >= total) return;
+    uint32_t at = upto - mine;
+    if (u >= at && u < upto)
+      over_mine([&](int i, const Seq& q) {
+        const uint32_t x = q.units(Hkv, of);
+        if (u >= at && u < at + x) {
           place[0] = i;
-          place[1] = u0 - at;
+          place[1] = u - at;
         }
-        at += u;
-      }
-    if (tid == 0) a.cut[blockIdx.x].parts = 0;
-    if (u0 >= total) return;
+        at += x;
+      });
     __syncthreads();
+    seq = __builtin_amdgcn_readfirstlane(place[0]);
+    in_seq = __builtin_amdgcn_readfirstlane(place[1]);
   }
-  unsigned long long u = blockIdx.x * share;
-  const unsigned long long end = u + share < total ? u + share : total;
-  int seq = (int)place[0];
-  unsigned long long in_seq = place[1];
+  const uint32_t end = u + share < total ? u + share : total;
 
   const int lds0 = (int)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * S::kRing;
   char* const ring = smem + wave * S::kRing;
@@ -142,9 +174,9 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
   while (u < end) {
     Seq q = sequence(a, seq, RT);
     while (q.tiles == 0) q = sequence(a, ++seq, RT);      // (u < total: there is one)
-    const uint32_t ht = divide(in_seq, q.steps), h = ht / q.tiles, tile = ht - h * q.tiles;
-    const int s0 = (int)(in_seq - (unsigned long long)ht * q.steps);
-    const int s1 = (int)(end - u < (unsigned long long)(q.steps - s0) ? s0 + (int)(end - u) : q.steps);
+    const uint32_t span = q.span(of), ht = in_seq / span, h = ht / q.tiles, tile = ht - h * q.tiles;
+    const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
+    const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
 
     // ---- the rows
     const int row0 = (int)tile * RT, pos0 = q.kv - q.q_len;
@@ -324,9 +356,9 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
       for (int dt = 0; dt < S::ND; ++dt) *(f32x4*)(meet + (wave * RT + r) * S::OS + 16 * dt + 4 * quarter) = o[mb][dt] * alpha;
     }
     __syncthreads();
-    const bool whole = s0 == 0 && s1 == q.steps;
+    const bool complete = s0 == 0 && s1 == q.steps;
     if (s0 == 0 && s1 < q.steps && tid == 0) {             // the shares that follow go on with it
-      const int more = (int)(((unsigned long long)(q.steps - s1) + share - 1) / share);
+      const int more = (int)((q.steps - s1 + share - 1) / share);
       a.cut[blockIdx.x] = Cut{1 + more, q.q0, (int)h, row0, min(RT, q.rows - row0)};
     }
     const long long slot = 2LL * blockIdx.x + (s0 == 0 ? 1 : 0);
@@ -342,7 +374,7 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
         v[0] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col);
         v[1] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col + 4);
       }
-      if (whole) {
+      if (complete) {
         const int tok = (int)a.by_g.div(row0 + r), head = (int)h * a.g + row0 + r - tok * a.g;
         const float inv = lt > 0.f ? 1.0f / lt : 0.f;
         bf16x8 out;
@@ -361,9 +393,9 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
       }
     }
     __syncthreads();
-    u += s1 - s0;
-    in_seq += s1 - s0;
-    if (in_seq >= q.units(Hkv)) {
+    u += units;
+    in_seq += units;
+    if (in_seq >= q.units(Hkv, of)) {
       ++seq;
       in_seq = 0;
     }
@@ -519,20 +551,24 @@ constexpr int kFewRows = 64;
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
 // and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
 struct Plan {
-  bool few, many;
+  bool few, many, fits;
   int mb, shares, slots, splits;
 };
 Plan plan_of(const CacheArgs& c) {
   const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
   Plan p;
-  p.many = (long long)most * g > kFewRows;
+  const long long cap = (long long)c.max_pages << c.page_log2, seen = c.window && c.window + (long long)most < cap ? c.window + (long long)most : cap;
+  // (steps are counted in 32 bits on the device)
+  const auto steps = [&](long long rows) { return (double)c.Hkv * (rows / 16 + c.n_seqs) * ((cap + kStep - 1) / kStep + 2048); };
+  const long long rows_all = (long long)c.n_tokens * g, rows_few = rows_all < (long long)c.n_seqs * kFewRows ? rows_all : (long long)c.n_seqs * kFewRows;
+  p.many = (long long)most * g > kFewRows || steps(rows_all) >= 4.0e9;
   p.few = !p.many || c.n_seqs > 1;
+  p.fits = !p.few || steps(p.many ? rows_few : rows_all) < 4.0e9;
   const int rows = p.many ? g : most * g;                // (beside prompts: single tokens, most likely)
   // Rows of a tile.  Larger tiles read K and V fewer times, smaller ones start and end sooner and are more of them.  28 / 4 heads, us with tiles of
   // 16 / 32 / 64 rows: 32 sequences x 8000 keys, 3 new tokens (21 rows) bf16 160 / 109 / 114, 8 bits 87 / 60 / 96; 8 new tokens (56 rows) 298 / 166 / 122
   // and 155 / 99 / 103; 200 x 500, 56 rows, 131 / 84 / 76 and 83 / 68 / 75; 2 x 300, 56 rows, 11.5 / 13.3 / 17.0 and 11.1 / 13.3 / 16.8; 1 x 2000 15.1 / 16.7 / 19.9.
   // So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
-  const long long cap = (long long)c.max_pages << c.page_log2, seen = c.window && c.window + (long long)most < cap ? c.window + (long long)most : cap;
   const bool small = (long long)c.n_seqs * c.Hkv * ((seen + kStep - 1) / kStep) <= 512;
   p.mb = rows <= 16 || small ? 1 : rows <= 32 || c.e4m3 ? 2 : 4;
   p.shares = 256 * per_cu(c.d, c.e4m3, p.mb);
@@ -583,7 +619,10 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
 
 }  // namespace
 
-size_t attend_cache_ws_bytes(const CacheArgs& c) { return workspace_of(c, plan_of(c)).total; }
+size_t attend_cache_ws_bytes(const CacheArgs& c) {
+  const Plan p = plan_of(c);
+  return p.fits ? workspace_of(c, p).total : 0;
+}
 
 hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float* lse, void* ws, hipStream_t st) {
   Args a;

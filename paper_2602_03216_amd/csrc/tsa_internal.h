@@ -168,7 +168,7 @@ struct CacheArgs {
 };
 hipError_t launch_cache_write(const CacheArgs& c, const void* K, const void* V, hipStream_t st);
 hipError_t launch_cache_read(const CacheArgs& c, int L, void* K, void* V, hipStream_t st);
-size_t attend_cache_ws_bytes(const CacheArgs& c);
+size_t attend_cache_ws_bytes(const CacheArgs& c);       // 0: more than the kernels can count
 hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float* lse, void* ws, hipStream_t st);
 
 }  // namespace tsa
