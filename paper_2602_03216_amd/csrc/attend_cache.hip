@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
 
   // ---- the share: thread t counts sequences t * per .. of the batch.  Where a few steps more than an equal share let no share go over the end of
   // a row tile, the tiles are counted as multiples of such a share: another tile in a share costs a meeting of the wavefronts and a start, which is
-  // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 EEE).
+  // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 28).
   // (Up to 64 sequences every wavefront does it for itself, a sequence per lane, without a barrier.)
   const bool alone = n <= 64;
   const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
@@ -404,16 +404,20 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
 
 constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
 
-// The sum of the parts of `R` rows: wavefront r finds row r's largest max and its sum, then groups of lanes take every G-th part of all of them.
-//   parts of row r: slot_of(part) + r of the arrays part_o [..][D] and part_ml [..][2];  out(r, col, v0, v1) gets two columns of a finished
-//   row, lse(r, value) its log-sum-exp.  rows: how many of the R there are.
-template <int D, int R, typename P, typename O, typename L>
-__device__ __forceinline__ void join_rows(const float* part_o, const float* part_ml, int parts, int rows, P&& slot_of, O&& out, L&& lse) {
-  constexpr int LPR = D / 4, G = 256 / LPR, kBatch = 8 / R;
-  static_assert(R == 1 || R == 4, "wavefronts are dealt over rows, or all take one");
+// Row tiles that a share's end cuts: the workgroup of the share that has a tile's first part, and a group of four of its rows.  The first part is
+// the second slot of its share, every later one the first slot of its share.  Wavefront r finds row r's largest max and its sum, then groups of
+// lanes take every G-th part of all four.
+template <int D>
+__global__ __launch_bounds__(256) void join_few_rows(Args a) {
+  constexpr int R = 4, LPR = D / 4, G = 256 / LPR, kBatch = 2;
   __shared__ float weight[R][kMostParts];
   __shared__ float meet[G][R][D];
-  __shared__ float ml[4][2];
+  __shared__ float ml[R][2];
+  const Cut c = a.cut[blockIdx.x];
+  const int r0 = R * blockIdx.y, rows = c.rows - r0, parts = c.parts;
+  if (parts == 0 || rows <= 0) return;
+  const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
+  const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
   f32x4 v[kBatch][R];
   const auto rows_from = [&](int w0) {
@@ -421,45 +425,29 @@ __device__ __forceinline__ void join_rows(const float* part_o, const float* part
     for (int i = 0; i < kBatch; ++i)
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
+        v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(a.part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
   };
   rows_from(grp);                                        // (the rows wait for nothing)
-  {
-    const int r = R == 1 ? 0 : wave, from = R == 1 ? tid : lane, step = R == 1 ? 256 : 64;
-    float m = kNone, l = 0.f;
-    if (r < rows)
-      for (int w = from; w < parts; w += step) {
-        const long long slot = slot_of(w) + r;
-        const float mp = part_ml[2 * slot], lp = part_ml[2 * slot + 1], mn = fmaxf(m, mp);
-        l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
-        m = mn;
-        weight[r][w] = mp;
-      }
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
+  float m = kNone, l = 0.f;
+  if (wave < rows)
+    for (int w = lane; w < parts; w += 64) {
+      const long long slot = slot_of(w) + wave;
+      const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1], mn = fmaxf(m, mp);
       l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
       m = mn;
+      weight[wave][w] = mp;
     }
-    if (lane == 0) {
-      ml[wave][0] = m;
-      ml[wave][1] = l;
-    }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
+    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+    m = mn;
+  }
+  if (lane == 0) {
+    ml[wave][0] = m;
+    ml[wave][1] = l;
   }
   __syncthreads();
-  float mt[R], lt[R];
-  if (R == 1) {
-    mt[0] = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
-    lt[0] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) lt[0] += ml[w][1] * fast_exp2(ml[w][0] - mt[0]);
-  } else {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      mt[r] = ml[r][0];
-      lt[r] = ml[r][1];
-    }
-  }
   f32x4 o[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
@@ -468,79 +456,79 @@ __device__ __forceinline__ void join_rows(const float* part_o, const float* part
     for (int i = 0; i < kBatch; ++i)
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - mt[r]);
+        if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - ml[r][0]);
     rows_from(w0 + kBatch * G);
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
   __syncthreads();
   for (int task = tid; task < R * D / 2; task += 256) {
-    const int r = task / (D / 2), c = 2 * (task % (D / 2));
+    const int r = task / (D / 2), x = 2 * (task % (D / 2));
     if (r >= rows) continue;
     float v0 = 0.f, v1 = 0.f;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      v0 += meet[g][r][c];
-      v1 += meet[g][r][c + 1];
+      v0 += meet[g][r][x];
+      v1 += meet[g][r][x + 1];
     }
-    float ls = lt[0], ms = mt[0];
-#pragma unroll
-    for (int k = 1; k < R; ++k)
-      if (r == k) { ls = lt[k]; ms = mt[k]; }
-    const float inv = ls > 0.f ? 1.0f / ls : 0.f;
-    out(r, c, v0 * inv, v1 * inv);
-    if (c == 0) lse(r, ls > 0.f ? (ms + log2f(ls)) * kLn2 : -INFINITY);
+    const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row), tok = c.q0 + k, head = c.head * a.g + row - k * a.g;
+    const float lt = ml[r][1], inv = lt > 0.f ? 1.0f / lt : 0.f;
+    bf16x2 out;
+    out[0] = (__bf16)(v0 * inv);
+    out[1] = (__bf16)(v1 * inv);
+    *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
+    if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
   }
 }
 
-// Row tiles that a share's end cuts: the workgroup of the share that has a tile's first part, and a group of four of its rows.  The first part is
-// the second slot of its share, every later one the first slot of its share.
-template <int D>
-__global__ __launch_bounds__(256) void join_few_rows(Args a) {
-  const Cut c = a.cut[blockIdx.x];
-  const int r0 = 4 * blockIdx.y;
-  if (c.parts == 0 || r0 >= c.rows) return;
-  const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
-  const auto where = [&](int r, int& tok, int& head) {
-    const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row);
-    tok = c.q0 + k;
-    head = c.head * a.g + row - k * a.g;
-  };
-  join_rows<D, 4>(a.part_o, a.part_ml, c.parts, c.rows - r0, [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; },
-                  [&](int r, int col, float v0, float v1) {
-                    int tok, head;
-                    where(r, tok, head);
-                    bf16x2 v;
-                    v[0] = (__bf16)v0;
-                    v[1] = (__bf16)v1;
-                    *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + col) = v;
-                  },
-                  [&](int r, float v) {
-                    int tok, head;
-                    where(r, tok, head);
-                    if (a.lse) a.lse[(long long)tok * a.Hq + head] = v;
-                  });
-}
-
-// Rows whose keys are cut into parts (many rows): one workgroup per token and query head.
+// Rows whose keys are cut into parts (many rows): a workgroup takes 16 rows of a row tile, D / 4 lanes a row, which they sum part by part.
 template <int D>
 __global__ __launch_bounds__(256) void join_many_rows(Args a) {
-  const int t = blockIdx.x, head = blockIdx.y, h = (int)a.by_g.div(head);
-  const int seq = sequence_of(a.b, t, threadIdx.x & 63);
+  constexpr int LPR = D / 4, G = 256 / LPR, kRows = 16, kBatch = 8;
+  const int lane = threadIdx.x & 63, grp = threadIdx.x / LPR, col = 4 * (threadIdx.x % LPR);
+  const int slot = blockIdx.x, h = blockIdx.y;
+  const int seq = last_up_to(a.b.n_seqs, slot, lane, [&](int i) { return first_slot(a, i); });
   if (seq < 0 || seq >= a.b.n_seqs) return;
-  const int q0 = a.b.first(seq), r = (t - q0) * a.g + head - h * a.g;
-  if (t < q0 || t >= a.b.first(seq + 1)) return;
-  const ManyTile x = many_tile(a, seq, r / kManyRows);
+  const ManyTile x = many_tile(a, seq, slot - first_slot(a, seq));
   if (!x.there || x.parts == 1) return;
-  const long long first = (((long long)first_slot(a, seq) + r / kManyRows) * a.b.Hkv + h) * a.splits * kManyRows + r % kManyRows;
-  join_rows<D, 1>(a.many_o, a.many_ml, x.parts, 1, [&](int w) -> long long { return first + (long long)w * kManyRows; },
-                  [&](int, int col, float v0, float v1) {
-                    bf16x2 v;
-                    v[0] = (__bf16)v0;
-                    v[1] = (__bf16)v1;
-                    *(bf16x2*)(a.O + t * a.o_t + head * a.o_h + col) = v;
-                  },
-                  [&](int, float v) { if (a.lse) a.lse[(long long)t * a.Hq + head] = v; });
+#pragma unroll
+  for (int k = 0; k < kRows; k += G) {
+    const int in_tile = kRows * blockIdx.z + k + grp, row = x.row0 + in_tile;
+    if (row >= x.rows) continue;
+    const long long first = ((long long)slot * a.b.Hkv + h) * a.splits * kManyRows + in_tile;
+    f32x4 o = {0, 0, 0, 0};
+    float m = kNone, l = 0.f;
+    for (int w0 = 0; w0 < x.parts; w0 += kBatch) {
+      f32x4 v[kBatch];
+      float mp[kBatch], lp[kBatch], mn = m;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const long long at = first + (long long)min(w0 + i, x.parts - 1) * kManyRows;
+        mp[i] = a.many_ml[2 * at];
+        lp[i] = a.many_ml[2 * at + 1];
+        v[i] = *(const f32x4*)(a.many_o + at * D + col);
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) mn = fmaxf(mn, mp[i]);
+      const float alpha = fast_exp2(m - mn);
+      m = mn;
+      l *= alpha;
+      o *= alpha;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float w = w0 + i < x.parts ? fast_exp2(mp[i] - mn) : 0.f;
+        l += lp[i] * w;
+        o += v[i] * w;
+      }
+    }
+    const int k_tok = (int)a.by_g.div(row), tok = x.q0 + k_tok, head = h * a.g + row - k_tok * a.g;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    bf16x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = (__bf16)(o[i] * inv);
+    *(bf16x4*)(a.O + tok * a.o_t + head * a.o_h + col) = out;
+    if (a.lse && col == 0) a.lse[(long long)tok * a.Hq + head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -611,7 +599,7 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.many && p.splits > 1) {
-    join_many_rows<D><<<dim3(a.b.n_tokens, a.Hq), 256, 0, st>>>(a);
+    join_many_rows<D><<<dim3(a.slots, a.b.Hkv, kManyRows / 16), 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;
