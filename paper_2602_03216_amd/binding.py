@@ -349,13 +349,17 @@ def tsa_sparse_layers(drift, delta=0.5):
     return list(out)
 
 
+# The handle of a device's current stream without the Python object around it, which costs 2.6 us of a call's 10.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _queue():
     """(handle of the current stream, current device)"""
     try:
-        st = torch.cuda.current_stream()
+        dev = torch.cuda.current_device()
+        return _raw_stream(dev), dev
     except (RuntimeError, AssertionError) as e:             # no GPU
         raise TsaError(TSA_ERR_HIP, str(e)) from None
-    return st.cuda_stream, st.device_index
 
 
 _BF16, _I32, _U8, _F32 = (torch.bfloat16,), (torch.int32,), (torch.uint8,), (torch.float32,)
