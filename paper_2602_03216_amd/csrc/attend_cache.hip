@@ -137,11 +137,14 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
   if (alone) {
     total = __shfl(upto, 63);
     if (u >= total) return;
-    seq = __ffsll((long long)__builtin_amdgcn_ballot_w64(u < upto)) - 1;
+    const unsigned long long behind = __builtin_amdgcn_ballot_w64(u < upto);
+    if (behind == 0) return;                             // (cu_q that does not ascend)
+    seq = __ffsll((long long)behind) - 1;
     in_seq = u - __builtin_amdgcn_readlane(upto - mine, seq);
   } else {
     __syncthreads();
     if (lane == 63) scan[wave] = upto;
+    if (tid == 0) place[0] = n;
     __syncthreads();
     total = 0;
     for (int w = 0; w < 4; ++w) {
@@ -172,8 +175,9 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
   const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
 
   while (u < end) {
-    Seq q = sequence(a, seq, RT);
-    while (q.tiles == 0) q = sequence(a, ++seq, RT);      // (u < total: there is one)
+    while (seq < n && sequence(a, seq, RT).tiles == 0) ++seq;
+    if (seq >= n) return;                                // (cu_q that does not ascend: the sums do not hold)
+    const Seq q = sequence(a, seq, RT);
     const uint32_t span = q.span(of), ht = in_seq / span, h = ht / q.tiles, tile = ht - h * q.tiles;
     const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
     const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
@@ -414,7 +418,7 @@ __global__ __launch_bounds__(256) void join_few_rows(Args a) {
   __shared__ float meet[G][R][D];
   __shared__ float ml[R][2];
   const Cut c = a.cut[blockIdx.x];
-  const int r0 = R * blockIdx.y, rows = c.rows - r0, parts = c.parts;
+  const int r0 = R * blockIdx.y, rows = c.rows - r0, parts = min(c.parts, (int)(gridDim.x - blockIdx.x));
   if (parts == 0 || rows <= 0) return;
   const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
   const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };

@@ -246,3 +246,22 @@ def test_a_pool_beyond_four_gigabytes(tsa):
     for h in range(2 * H):
         want, _, mag = srv.attend(q[:, h], orc.bf16_to_f64(K[:, h // 2]), orc.bf16_to_f64(V[:, h // 2]), np.ones(kv, dtype=bool), d ** -0.5)
         assert (np.abs(got[:, h] - want) <= (2.0 ** -8 + 2.0 ** -12) * mag + 2.0 ** -8 * np.abs(want)).all()
+
+
+def test_lengths_that_do_not_fit(tsa):
+    """Lengths beyond the table, negative ones, new tokens beyond the rows there are: every access stays inside the tensors, and the sequences that
+    are as described are right."""
+    b = Batch(7200, [1, 3, 200], [90, 40, 260], 8, 2, 128, 16)
+    want, want_lse = b.run(tsa)
+    desc = b.desc(tsa)
+    guard = 64
+    rows = torch.full((b.T + 2 * guard, b.Hq, b.d), 7.0, dtype=torch.bfloat16, device=gu.DEV)
+    O = rows[guard:guard + b.T]
+    ws = tsa.alloc_attend_cache_workspace(desc)
+    for kv, cu in (([1 << 30, 40, 260], b.cu), ([90, -5, 260], b.cu), ([90, 40, 1 << 29], b.cu), (b.kv, [0, 1, 4, 1 << 30])):
+        tsa.tsa_attend_cache(desc, gu.to_dev(b.q), *b.pools, ints(cu), ints(kv), ints(b.tab), O, ws)
+        assert (rows[:guard] == 7).all() and (rows[guard + b.T:] == 7).all()
+        for i in range(3):
+            if kv[i] == b.kv[i] and cu[i + 1] == b.cu[i + 1]:
+                cut = slice(b.cu[i], b.cu[i + 1])
+                assert (O[cut].double() - want[cut].double()).abs().max() <= 2.0 ** -6      # (another partition of the keys: other roundings)
