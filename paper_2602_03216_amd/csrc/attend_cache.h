@@ -115,6 +115,7 @@ __device__ __forceinline__ int first_slot(const Args& a, int seq) { return a.b.f
 }  // namespace attend_cache_detail
 
 // attend_cache_many.hip: sets the grid's part of the arguments
-hipError_t launch_attend_many(attend_cache_detail::Args& a, int d, bool e4m3, hipStream_t st);
+// shares: workgroups for the sequences with few rows (tiles of 16) in the same launch, or 0
+hipError_t launch_attend_many(attend_cache_detail::Args& a, int d, bool e4m3, int shares, hipStream_t st);
 
 }  // namespace tsa

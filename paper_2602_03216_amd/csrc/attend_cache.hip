@@ -1,23 +1,6 @@
-// Attention of the new tokens of a ragged batch over the paged cache:
-//   o_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j of t's sequence with p_t - window < j <= p_t.
-//
-// The g query heads of a KV head and the new tokens of a sequence are the rows of one matrix: row r is token r / g, head r % g of
-// the group, so K and V are read once for all of them.
-//
-// Few rows per sequence (single tokens, drafted tokens): K and V are what has to be read, HBM bounds it, and the keys are the axis that
-// fills the chip.  The work of the whole batch, counted in steps of 128 keys of one (sequence, KV head, tile of 16 rows), is cut into
-// equal shares, one per workgroup; lengths are known on the device only, so every workgroup sums them up itself and finds its
-// place.  A share that covers only a part of a row tile's keys leaves its running max, sum and output in the workspace, and a second launch
-// joins them; whole ones are written at once.
-//   A wavefront takes 32 keys of a step, with a softmax of its own; the four meet at the end of a segment.  S^T = K Q^T on
-// v_mfma_f32_16x16x32_bf16: rows = keys, columns = the tile's rows, so a lane keeps one row's max and sum.  K goes from memory straight
-// into the registers of that product (a lane's 16 bytes are its operand).  O^T = V^T P^T takes the probabilities as the lane holds them: its
-// contraction index runs over keys 4 q .. 4 q + 3 of the first 16 and of the second 16 keys (q = lane / 16), and V^T comes out of LDS
-// by the transposing reads, four (eight in 8 bits) keys of one column per lane.  V goes to LDS without passing registers; the
-// next step's K and V are in flight while a step is computed, and no wavefront waits for another inside a segment.
-//   8 bits: K is widened to bf16 with its row's power of two by the conversion (exact), V without it, and V's power goes into the
-// probability in front of its rounding.
-#include "attend_cache.h"
+// Attention over the paged cache: the launches of a call, and the joining of parts.  Sequences with few rows: attend_cache_few.h, with many:
+// attend_cache_many.hip.
+#include "attend_cache_few.h"
 
 namespace tsa {
 
@@ -26,384 +9,10 @@ using namespace attend_cache_detail;
 
 namespace {
 
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// What a sequence asks for.
-struct Seq {
-  int q0, q_len, kv, rows, tiles, first, steps;          // first: its first key that any query sees, rounded down to 16
-  // steps of all its row tiles, each counted as a multiple of `of`
-  __device__ __forceinline__ uint32_t units(int Hkv, int of) const { return (uint32_t)(Hkv * tiles) * span(of); }
-  __device__ __forceinline__ uint32_t span(int of) const { return of == 1 ? steps : (uint32_t)((steps + of - 1) / of) * of; }
-};
-
-__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) {
-  Seq s;
-  s.q0 = a.b.first(i);
-  s.q_len = max(a.b.first(i + 1) - s.q0, 0);
-  s.kv = a.b.kv(i);
-  s.rows = s.q_len * a.g;
-  if (s.rows > a.few) s.rows = 0;
-  s.tiles = (s.rows + rt - 1) / rt;
-  s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
-  s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
-  return s;
-}
-
-// Shares per CU, all of which run at once.  What they have in flight together is what the memory rate comes from: the rows of d = 64 in 8 bits
-// are short and take four (300 sequences x 1000 keys, 8 KV heads: 97 -> 81 us, 6 x 131072 158 -> 151); with longer rows two have enough in
-// flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 195 us with two, 207 with three; bf16, d = 64: 189 with two, 195 with four).
-constexpr int per_cu(int d, bool e4m3, int mb) { return mb == 4 && d == 128 ? 1 : mb == 1 && d == 64 && e4m3 ? 4 : 2; }
-
-template <int D, bool E4M3, int MB>
-struct Shape {
-  static constexpr int RT = 16 * MB;                     // rows of a tile
-  static constexpr int kPerCU = per_cu(D, E4M3, MB), kShares = 256 * kPerCU;
-  static constexpr int RB = E4M3 ? D : 2 * D;            // bytes of a cached row
-  static constexpr int LPR = RB / 16, RPI = 64 / LPR;    // lanes per row, rows of a load into LDS
-  static constexpr int NK = RB / 64;                     // 16-byte pieces of a row of K per lane
-  static constexpr int NS = D / 32, ND = D / 16;         // k-steps of the first product, column tiles of the second
-  static constexpr int kRing = 2 * 32 * RB;              // LDS bytes of a wavefront: two steps of V
-  static constexpr int OS = D + 4;                       // floats between rows where the wavefronts meet
-  static constexpr int kMerge = 4 * RT * OS * 4;
-  static constexpr int kLds = 4 * kRing > kMerge ? 4 * kRing : kMerge;
-  // 16-byte piece p of row r of V is kept at p ^ swizzle(r): the 32 lanes that a transposing read serves at once then touch all banks
-  __device__ static __forceinline__ int swizzle(int r) {
-    if (!E4M3) return RB == 256 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
-    return RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1;
-  }
-};
-
-// K of a step in registers, and the exponents of both.
-template <int NK>
-struct StepRegs {
-  u32x4 k[2][NK];
-  uint32_t ks[2], vs[2];
-};
-
 template <int D, bool E4M3, int MB>
 __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args a) {
-  using S = Shape<D, E4M3, MB>;
-  constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
-  __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
-  __shared__ float ml[4][RT][2];
-  __shared__ uint32_t scan[4], place[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
-  const int n = a.b.n_seqs, Hkv = a.b.Hkv;
-
-  // ---- the share: thread t counts sequences t * per .. of the batch.  Where a few steps more than an equal share let no share go over the end of
-  // a row tile, the tiles are counted as multiples of such a share: another tile in a share costs a meeting of the wavefronts and a start, which is
-  // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 28).
-  // (Up to 64 sequences every wavefront does it for itself, a sequence per lane, without a barrier.)
-  const bool alone = n <= 64;
-  const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
-  const Seq own = sequence(a, min(i0, n - 1), RT);
-  const auto over_mine = [&](auto&& f) {
-    for (int i = i0; i < i1; ++i) f(i, per == 1 ? own : sequence(a, i, RT));
-  };
-  const auto sum_up = [&](uint32_t x) -> uint32_t {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    if (alone) return x;
-    __syncthreads();
-    if (lane == 0) scan[wave] = x;
-    __syncthreads();
-    return scan[0] + scan[1] + scan[2] + scan[3];
-  };
-  uint32_t mine = 0;
-  over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
-  uint32_t total = sum_up(mine), share = (total + kShares - 1) / kShares;
-  int of = 1;
-  if (share > 1) {
-    for (int k = 0; k < 4 && of == 1; ++k) {
-      uint32_t parts = 0;                                // shares that whole ones of share + k steps make
-      over_mine([&](int, const Seq& q) { parts += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k - 1) / (share + k)); });
-      if (sum_up(parts) <= (uint32_t)kShares) of = (int)share + k;
-    }
-    if (of > 1) {
-      share = of;
-      mine = 0;
-      over_mine([&](int, const Seq& q) { mine += q.units(Hkv, of); });
-    }
-  }
-  if (tid == 0) a.cut[blockIdx.x].parts = 0;
-  uint32_t upto = mine;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint32_t o = __shfl_up(upto, m);
-    if (lane >= m) upto += o;
-  }
-  uint32_t u = blockIdx.x * share, in_seq;
-  int seq;
-  if (alone) {
-    total = __shfl(upto, 63);
-    if (u >= total) return;
-    const unsigned long long behind = __builtin_amdgcn_ballot_w64(u < upto);
-    if (behind == 0) return;                             // (cu_q that does not ascend)
-    seq = __ffsll((long long)behind) - 1;
-    in_seq = u - __builtin_amdgcn_readlane(upto - mine, seq);
-  } else {
-    __syncthreads();
-    if (lane == 63) scan[wave] = upto;
-    if (tid == 0) place[0] = n;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) upto += scan[w];
-      total += scan[w];
-    }
-    if (u >= total) return;
-    uint32_t at = upto - mine;
-    if (u >= at && u < upto)
-      over_mine([&](int i, const Seq& q) {
-        const uint32_t x = q.units(Hkv, of);
-        if (u >= at && u < at + x) {
-          place[0] = i;
-          place[1] = u - at;
-        }
-        at += x;
-      });
-    __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(place[0]);
-    in_seq = __builtin_amdgcn_readfirstlane(place[1]);
-  }
-  const uint32_t end = u + share < total ? u + share : total;
-
-  const int lds0 = (int)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * S::kRing;
-  char* const ring = smem + wave * S::kRing;
-  // transposing reads: this lane's address in a step's V, up to the column tile (an exclusive or) and, in bf16, the second 16 keys
-  const int v_row = E4M3 ? 4 * quarter + ((lo >> 1) & 3) + ((lo >> 3) << 4) : 4 * quarter + (lo >> 2);
-  const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
-
-  while (u < end) {
-    while (seq < n && sequence(a, seq, RT).tiles == 0) ++seq;
-    if (seq >= n) return;                                // (cu_q that does not ascend: the sums do not hold)
-    const Seq q = sequence(a, seq, RT);
-    const uint32_t span = q.span(of), ht = in_seq / span, h = ht / q.tiles, tile = ht - h * q.tiles;
-    const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
-    const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
-
-    // ---- the rows
-    const int row0 = (int)tile * RT, pos0 = q.kv - q.q_len;
-    const int p_min = pos0 + (int)a.by_g.div(row0), p_max = pos0 + (int)a.by_g.div(min(row0 + RT, q.rows) - 1);
-    const int see_lo = a.window ? max(0, p_min - a.window + 1) : 0, see_hi = p_max + 1;     // keys that some row of the tile sees
-    const int all_lo = a.window ? p_max - a.window + 1 : 0;                                 // keys all_lo .. p_min are seen by all of them
-    bf16x8 qf[MB][S::NS];
-    int pos[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      const int r = min(row0 + 16 * mb + lo, q.rows - 1), tok = (int)a.by_g.div(r);
-      pos[mb] = pos0 + tok;
-      const __bf16* src = a.Q + (q.q0 + tok) * a.q_t + ((int)h * a.g + r - tok * a.g) * a.q_h;
-#pragma unroll
-      for (int st = 0; st < S::NS; ++st)
-        qf[mb][st] = *(const bf16x8*)(src + (E4M3 ? 64 * (st >> 1) + 16 * quarter + 8 * (st & 1) : 32 * st + 8 * quarter));
-    }
-
-    // ---- pages: lane l holds the id of the 16 keys from 16 (64 chunk + l) on, counted from q.first
-    auto page_ids = [&](int chunk) -> int {
-      const int key = q.first + 16 * (64 * chunk + lane);
-      return key < see_hi ? a.b.page(seq, key) : -1;
-    };
-    int chunk = s0 >> 3, ids = page_ids(chunk), ids_next = page_ids(chunk + 1);
-    auto issue = [&](int s, StepRegs<S::NK>& x, int buf) {
-      if ((s >> 3) != chunk) {
-        ++chunk;
-        ids = ids_next;
-        ids_next = page_ids(chunk + 1);
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int id = __builtin_amdgcn_readlane(ids, (8 * s + 2 * wave + j) & 63);
-        const int key0 = q.first + 16 * (8 * s + 2 * wave + j);
-        const long long row = a.b.row(max(id, 0), (int)h, key0);
-        const char* kr = a.kp + (row + lo) * RB + 16 * quarter;
-#pragma unroll
-        for (int i = 0; i < S::NK; ++i) x.k[j][i] = *(const u32x4*)(kr + 64 * i);
-        if (E4M3) {
-          x.ks[j] = a.ks[row + lo];
-          x.vs[j] = *(const uint32_t*)(a.vs + row + 4 * quarter);
-        }
-#pragma unroll
-        for (int i = 0; i < 16 / S::RPI; ++i) {
-          const int r = i * S::RPI + lane / S::LPR, piece = (lane % S::LPR) ^ S::swizzle(16 * j + r);
-          const bool seen = id >= 0 && key0 + r >= see_lo && key0 + r < see_hi;
-          load_row_to_lds((seen ? a.vp + (row + r) * RB : (const char*)g_zeros) + 16 * piece, lds0 + buf * (32 * RB) + (16 * j + i * S::RPI) * RB);
-        }
-      }
-    };
-
-    f32x4 o[MB][S::ND];
-    float m[MB], l[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      m[mb] = kNone;
-      l[mb] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < S::ND; ++dt) o[mb][dt] = f32x4{0, 0, 0, 0};
-    }
-
-    auto compute = [&](int s, int ids_s, const StepRegs<S::NK>& x, int buf) {
-      const int key0 = q.first + 16 * (8 * s + 2 * wave);
-      bool masked[2], dead[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int k0 = key0 + 16 * j;
-        const bool gone = __builtin_amdgcn_readlane(ids_s, (8 * s + 2 * wave + j) & 63) < 0;
-        dead[j] = gone || k0 >= see_hi || k0 + 15 < see_lo;
-        masked[j] = dead[j] || k0 + 15 > p_min || k0 < all_lo;
-      }
-      if (dead[0] && dead[1]) return;
-      f32x4 sc[MB][2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) sc[mb][j] = f32x4{0, 0, 0, 0};
-        const float k_scale = E4M3 ? exponent_value(x.ks[j]) : 1.0f;
-#pragma unroll
-        for (int st = 0; st < S::NS; ++st) {
-          bf16x8 kf;
-          if (E4M3) kf = widen8(x.k[j][st >> 1][2 * (st & 1)], x.k[j][st >> 1][2 * (st & 1) + 1], k_scale);
-          else kf = __builtin_bit_cast(bf16x8, x.k[j][st]);
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb) sc[mb][j] = mfma16(kf, qf[mb][st], sc[mb][j]);
-        }
-        if (masked[j]) {
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int key = key0 + 16 * j + 4 * quarter + r;
-              if (dead[j] || key > pos[mb] || (a.window && key <= pos[mb] - a.window)) sc[mb][j][r] = -INFINITY;
-            }
-        }
-      }
-      bf16x8 pf[MB];
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        float mx = sc[mb][0][0];
-#pragma unroll
-        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, sc[mb][r >> 2][r & 3]);
-        mx *= a.c;
-        if (__any(mx > m[mb] + kLag)) {
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const float mn = fmaxf(m[mb], mx), alpha = fast_exp2(m[mb] - mn);
-          m[mb] = mn;
-          l[mb] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[mb][dt][r] *= alpha;
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = fast_exp2(fmaf(sc[mb][j][r], a.c, -m[mb]));
-            l[mb] += p;
-            // (bf16 for the product, as the other attention kernels have it; V's power of two is exact.  A byte of a row that nobody
-            // has written may say infinity, next to a probability of 0.)
-            pf[mb][4 * j + r] = (__bf16)(E4M3 ? p * fminf(exponent_value((x.vs[j] >> (8 * r)) & 0xffu), 0x1p127f) : p);
-          }
-      }
-#pragma unroll
-      for (int dt = 0; dt < S::ND; ++dt) {
-        bf16x8 vf;
-        if (E4M3) {
-          typedef __attribute__((ext_vector_type(2))) int i32x2;
-          const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(ring + buf * (32 * RB) + (v_rd ^ (dt << 4))));
-          vf = widen8((uint32_t)w[0], (uint32_t)w[1], 1.0f);
-        } else {
-          const char* at = ring + buf * (32 * RB) + (v_rd ^ (dt << 5));
-          const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)at);
-          const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(at + 16 * RB));
-          vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) o[mb][dt] = mfma16(vf, pf[mb], o[mb][dt]);
-      }
-    };
-
-    StepRegs<S::NK> xa, xb;
-    issue(s0, xa, 0);
-    for (int s = s0;; s += 2) {
-      wait_all();
-      int ids_s = ids;
-      if (s + 1 < s1) issue(s + 1, xb, 1);
-      compute(s, ids_s, xa, 0);
-      if (s + 1 >= s1) break;
-      wait_all();
-      ids_s = ids;
-      if (s + 2 < s1) issue(s + 2, xa, 0);
-      compute(s + 1, ids_s, xb, 1);
-      if (s + 2 >= s1) break;
-    }
-
-    // ---- the four wavefronts meet
-    __syncthreads();                                     // (the rings are free)
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      l[mb] += __shfl_xor(l[mb], 16);
-      l[mb] += __shfl_xor(l[mb], 32);
-      if (quarter == 0) {
-        ml[wave][16 * mb + lo][0] = m[mb];
-        ml[wave][16 * mb + lo][1] = l[mb];
-      }
-    }
-    __syncthreads();
-    float* const meet = (float*)smem;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      const int r = 16 * mb + lo;
-      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0])), alpha = fast_exp2(m[mb] - mt);
-#pragma unroll
-      for (int dt = 0; dt < S::ND; ++dt) *(f32x4*)(meet + (wave * RT + r) * S::OS + 16 * dt + 4 * quarter) = o[mb][dt] * alpha;
-    }
-    __syncthreads();
-    const bool complete = s0 == 0 && s1 == q.steps;
-    if (s0 == 0 && s1 < q.steps && tid == 0) {             // the shares that follow go on with it
-      const int more = (int)((q.steps - s1 + share - 1) / share);
-      a.cut[blockIdx.x] = Cut{1 + more, q.q0, (int)h, row0, min(RT, q.rows - row0)};
-    }
-    const long long slot = 2LL * blockIdx.x + (s0 == 0 ? 1 : 0);
-    for (int task = tid; task < RT * (D / 8); task += 256) {
-      const int r = task / (D / 8), col = 8 * (task % (D / 8));
-      if (row0 + r >= q.rows) continue;
-      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0]));
-      float lt = 0.f;
-      f32x4 v[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        lt += ml[w][r][1] * fast_exp2(ml[w][r][0] - mt);
-        v[0] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col);
-        v[1] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col + 4);
-      }
-      if (complete) {
-        const int tok = (int)a.by_g.div(row0 + r), head = (int)h * a.g + row0 + r - tok * a.g;
-        const float inv = lt > 0.f ? 1.0f / lt : 0.f;
-        bf16x8 out;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = (__bf16)(v[i >> 2][i & 3] * inv);
-        *(bf16x8*)(a.O + (q.q0 + tok) * a.o_t + head * a.o_h + col) = out;
-        if (a.lse && col == 0) a.lse[(long long)(q.q0 + tok) * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
-      } else {
-        float* dst = a.part_o + (slot * RT + r) * D + col;
-        *(f32x4*)dst = v[0];
-        *(f32x4*)(dst + 4) = v[1];
-        if (col == 0) {
-          a.part_ml[(slot * RT + r) * 2] = mt;
-          a.part_ml[(slot * RT + r) * 2 + 1] = lt;
-        }
-      }
-    }
-    __syncthreads();
-    u += units;
-    in_seq += units;
-    if (in_seq >= q.units(Hkv, of)) {
-      ++seq;
-      in_seq = 0;
-    }
-  }
+  __shared__ __attribute__((aligned(1024))) char smem[Shape<D, E4M3, MB>::kLds];
+  few_rows<D, E4M3, MB>(a, smem, blockIdx.x);
 }
 
 constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
@@ -418,70 +27,74 @@ __global__ __launch_bounds__(256) void join_few_rows(Args a) {
   __shared__ float meet[G][R][D];
   __shared__ float ml[R][2];
   const Cut c = a.cut[blockIdx.x];
-  const int r0 = R * blockIdx.y, rows = c.rows - r0, parts = min(c.parts, (int)(gridDim.x - blockIdx.x));
-  if (parts == 0 || rows <= 0) return;
-  const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
-  const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
-  f32x4 v[kBatch][R];
-  const auto rows_from = [&](int w0) {
+  const int parts = min(c.parts, (int)(gridDim.x - blockIdx.x));
+  if (parts == 0) return;
+  for (int r0 = R * blockIdx.y; r0 < c.rows; r0 += R * gridDim.y) {
+    const int rows = c.rows - r0;
+    const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
+    const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
+    f32x4 v[kBatch][R];
+    const auto rows_from = [&](int w0) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i)
+      for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-        v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(a.part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
-  };
-  rows_from(grp);                                        // (the rows wait for nothing)
-  float m = kNone, l = 0.f;
-  if (wave < rows)
-    for (int w = lane; w < parts; w += 64) {
-      const long long slot = slot_of(w) + wave;
-      const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1], mn = fmaxf(m, mp);
+        for (int r = 0; r < R; ++r)
+          v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(a.part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
+    };
+    rows_from(grp);                                        // (the rows wait for nothing)
+    float m = kNone, l = 0.f;
+    if (wave < rows)
+      for (int w = lane; w < parts; w += 64) {
+        const long long slot = slot_of(w) + wave;
+        const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1], mn = fmaxf(m, mp);
+        l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+        m = mn;
+        weight[wave][w] = mp;
+      }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
       l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
       m = mn;
-      weight[wave][w] = mp;
+    }
+    if (lane == 0) {
+      ml[wave][0] = m;
+      ml[wave][1] = l;
+    }
+    __syncthreads();
+    f32x4 o[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
+    for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - ml[r][0]);
+      rows_from(w0 + kBatch * G);
     }
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) {
-    const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
-    l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
-    m = mn;
-  }
-  if (lane == 0) {
-    ml[wave][0] = m;
-    ml[wave][1] = l;
-  }
-  __syncthreads();
-  f32x4 o[R];
+    for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
+    __syncthreads();
+    for (int task = tid; task < R * D / 2; task += 256) {
+      const int r = task / (D / 2), x = 2 * (task % (D / 2));
+      if (r >= rows) continue;
+      float v0 = 0.f, v1 = 0.f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
-  for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - ml[r][0]);
-    rows_from(w0 + kBatch * G);
-  }
-#pragma unroll
-  for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
-  __syncthreads();
-  for (int task = tid; task < R * D / 2; task += 256) {
-    const int r = task / (D / 2), x = 2 * (task % (D / 2));
-    if (r >= rows) continue;
-    float v0 = 0.f, v1 = 0.f;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      v0 += meet[g][r][x];
-      v1 += meet[g][r][x + 1];
+      for (int g = 0; g < G; ++g) {
+        v0 += meet[g][r][x];
+        v1 += meet[g][r][x + 1];
+      }
+      const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row), tok = c.q0 + k, head = c.head * a.g + row - k * a.g;
+      const float lt = ml[r][1], inv = lt > 0.f ? 1.0f / lt : 0.f;
+      bf16x2 out;
+      out[0] = (__bf16)(v0 * inv);
+      out[1] = (__bf16)(v1 * inv);
+      *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
+      if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
     }
-    const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row), tok = c.q0 + k, head = c.head * a.g + row - k * a.g;
-    const float lt = ml[r][1], inv = lt > 0.f ? 1.0f / lt : 0.f;
-    bf16x2 out;
-    out[0] = (__bf16)(v0 * inv);
-    out[1] = (__bf16)(v1 * inv);
-    *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
-    if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
+    __syncthreads();
   }
 }
 
@@ -544,7 +157,7 @@ constexpr int kFewRows = 64;
 // and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
 struct Plan {
   bool few, many, fits;
-  int mb, shares, slots, splits;
+  int mb, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
 };
 Plan plan_of(const CacheArgs& c) {
   const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
@@ -563,6 +176,7 @@ Plan plan_of(const CacheArgs& c) {
   // So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
   const bool small = (long long)c.n_seqs * c.Hkv * ((seen + kStep - 1) / kStep) <= 512;
   p.mb = rows <= 16 || small ? 1 : rows <= 32 || c.e4m3 ? 2 : 4;
+  p.rows = !p.many && most * g < 16 * p.mb ? most * g : 16 * p.mb;
   p.shares = 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
   const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
@@ -593,13 +207,17 @@ template <int D, bool E4M3>
 hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
   hipError_t e;
   a.few = p.many ? (p.few ? kFewRows : 0) : 0x7fffffff;
-  if (p.many && (e = launch_attend_many(a, D, E4M3, st)) != hipSuccess) return e;
-  if (p.few) {
+  // with tiles of 16 rows the shares run in the same launch as the rows of many, behind them: in its tail
+  const bool both = p.many && p.few && p.mb == 1;
+  if (p.many && (e = launch_attend_many(a, D, E4M3, both ? p.shares : 0, st)) != hipSuccess) return e;
+  if (p.few && !both) {
     if (p.mb == 1) attend_few_rows<D, E4M3, 1><<<p.shares, 256, 0, st>>>(a);
     else if (p.mb == 2) attend_few_rows<D, E4M3, 2><<<p.shares, 256, 0, st>>>(a);
     else attend_few_rows<D, E4M3, 4><<<p.shares, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    join_few_rows<D><<<dim3(p.shares, 4 * p.mb), 256, 0, st>>>(a);
+  }
+  if (p.few) {
+    join_few_rows<D><<<dim3(p.shares, (p.rows + 3) / 4), 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.many && p.splits > 1) {

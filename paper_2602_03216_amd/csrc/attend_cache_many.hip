@@ -10,7 +10,7 @@
 // register that holds the ids of 64 blocks.  8-bit rows pass the registers, where the conversion widens them to bf16 with their power of two
 // (exact): 32 conversions per wavefront and tile beside 32 products; the loop is then the same.
 //   Where the row tiles of a call do not fill the chip their keys are cut into parts, joined by a second launch.
-#include "attend_cache.h"
+#include "attend_cache_few.h"
 
 namespace tsa {
 
@@ -47,11 +47,20 @@ struct Staged {
   uint32_t e[CH8];
 };
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a) {
+// FEW: the workgroups behind the first `grid` ones are shares of the sequences with few rows.
+template <int D, bool E4M3, bool FEW>
+__global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned grid) {
   using T = Tiles<D, E4M3>;
   constexpr int NS = T::NS, ND = T::ND, RB = T::RB, ROWB = T::ROWB;
-  __shared__ __attribute__((aligned(1024))) char smem[5 * T::KHALF + 2 * T::VTILE];     // K in a ring of five half tiles, V of two tiles
+  constexpr int kRings = 5 * T::KHALF + 2 * T::VTILE;    // K in a ring of five half tiles, V of two tiles
+  constexpr int kFewLds = FEW ? Shape<D, E4M3, 1>::kLds : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[kRings > kFewLds ? kRings : kFewLds];
+  if constexpr (FEW) {
+    if (blockIdx.x >= grid) {
+      few_rows<D, E4M3, 1>(a, smem, blockIdx.x - grid);
+      return;
+    }
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 31, hi = lane >> 5;
 
   // ---- workgroup -> KV head, row tile, part.  id % 8 is the XCD: the row tiles of a head stay on one (or a few) of them, the last ones first.
@@ -413,7 +422,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a) {
     return;
   }
   using Out = attend_detail::RowOut<D, ND, false>;
-  static_assert(NW * Out::kLds <= (int)sizeof(smem), "the rows of all wavefronts fit the tile rings");
+  static_assert(NW * Out::kLds <= kRings, "the rows of all wavefronts fit the tile rings");
   char* const lds_out = smem + wave * Out::kLds;
   Out out;
   out.put(o[0], lt > 0.f ? 1.0f / lt : 0.f, lds_out, lane);
@@ -432,22 +441,32 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a) {
 
 }  // namespace
 
-hipError_t launch_attend_many(Args& a, int d, bool e4m3, hipStream_t st) {
+namespace {
+
+template <int D, bool E4M3>
+void launch_rows(const Args& a, unsigned grid, int shares, hipStream_t st) {
+  if (shares) attend_many_rows<D, E4M3, true><<<grid + shares, 64 * NW, 0, st>>>(a, grid);
+  else attend_many_rows<D, E4M3, false><<<grid, 64 * NW, 0, st>>>(a, grid);
+}
+
+}  // namespace
+
+hipError_t launch_attend_many(Args& a, int d, bool e4m3, int shares, hipStream_t st) {
   // KV heads over the XCDs; where their number is no multiple of 8, every head is cut into alternating items
   int gcd = 8, log2 = 0;
   while (a.b.Hkv % gcd) { gcd >>= 1; ++log2; }
   a.split_log2 = log2;
   a.vheads_per_xcd = a.b.Hkv / gcd;
   const long long items = (long long)a.slots * a.splits, ranks = (items + (1 << log2) - 1) >> log2, grid = 8LL * a.vheads_per_xcd * ranks;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (grid + shares > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   a.by_vheads = FastDiv((uint32_t)a.vheads_per_xcd, (uint64_t)a.vheads_per_xcd * (ranks + 1));
   a.by_splits = FastDiv((uint32_t)a.splits, (uint64_t)items + 8);
   if (d == 128) {
-    if (e4m3) attend_many_rows<128, true><<<(unsigned)grid, 64 * NW, 0, st>>>(a);
-    else attend_many_rows<128, false><<<(unsigned)grid, 64 * NW, 0, st>>>(a);
+    if (e4m3) launch_rows<128, true>(a, (unsigned)grid, shares, st);
+    else launch_rows<128, false>(a, (unsigned)grid, shares, st);
   } else {
-    if (e4m3) attend_many_rows<64, true><<<(unsigned)grid, 64 * NW, 0, st>>>(a);
-    else attend_many_rows<64, false><<<(unsigned)grid, 64 * NW, 0, st>>>(a);
+    if (e4m3) launch_rows<64, true>(a, (unsigned)grid, shares, st);
+    else launch_rows<64, false>(a, (unsigned)grid, shares, st);
   }
   return hipGetLastError();
 }
