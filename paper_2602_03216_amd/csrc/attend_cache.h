@@ -52,12 +52,18 @@ struct Args {
   FastDiv by_vheads, by_splits;
 };
 
+// The same in all lanes, and kept in a scalar: the compiler forms quotients, and what is loaded or shuffled, in vector registers, and leaves everything
+// that follows from them there: addresses, loop counts and branches, some thirty registers of a kernel.
+__device__ __forceinline__ int one(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // 64 lanes' 16 bytes to LDS bytes lds .. lds + 1023.  Counted by vmcnt and by nothing that the compiler tracks; no output register.  The wait
-// states: m0 may come out of a vector instruction.
+// states: m0 may come out of a vector instruction.  ONCE: the bytes are not kept in the caches.
+template <bool ONCE = false>
 __device__ __forceinline__ void load_row_to_lds(const void* p, int lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
   lds = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
+  if (ONCE) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off nt" ::"{m0}"(lds), "v"(p) : "memory");
+  else asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
 #endif
 }
 // Everything that this wavefront asked for has landed, in registers and in LDS, and its LDS reads are done.
@@ -90,22 +96,22 @@ struct ManyTile {
 };
 __device__ __forceinline__ ManyTile many_tile(const Args& a, int seq, int tile) {
   ManyTile x;
-  x.q0 = a.b.first(seq);
-  x.q_len = max(a.b.first(seq + 1) - x.q0, 0);
-  x.kv = a.b.kv(seq);
+  x.q0 = one(a.b.first(seq));
+  x.q_len = max(one(a.b.first(seq + 1)) - x.q0, 0);
+  x.kv = one(a.b.kv(seq));
   x.rows = x.q_len * a.g;
   x.row0 = tile * kManyRows;
   x.there = x.rows > a.few && x.row0 < x.rows;
   const int pos0 = x.kv - x.q_len;
-  x.p_min = pos0 + (int)a.by_g.div(max(0, min(x.row0, x.rows - 1)));
-  x.p_max = pos0 + (int)a.by_g.div(max(0, min(x.row0 + kManyRows, x.rows) - 1));
+  x.p_min = pos0 + one(a.by_g.div(max(0, min(x.row0, x.rows - 1))));
+  x.p_max = pos0 + one(a.by_g.div(max(0, min(x.row0 + kManyRows, x.rows) - 1)));
   x.see_lo = a.window ? max(0, x.p_min - a.window + 1) : 0;
   x.see_hi = x.p_max + 1;
   x.start = x.see_lo & ~15;
   x.tiles = max(0, (x.see_hi - x.start + kTile - 1) / kTile);
   const int parts = max(1, min(a.splits, x.tiles / kPartTiles));
-  x.per = (x.tiles + parts - 1) / parts;
-  x.parts = x.per ? (x.tiles + x.per - 1) / x.per : 1;
+  x.per = one((x.tiles + parts - 1) / parts);
+  x.parts = one(x.per ? (x.tiles + x.per - 1) / x.per : 1);
   return x;
 }
 // First slot of a sequence's row tiles in the grid: rows in front of it, in tiles, and one more for every sequence, which is never less than

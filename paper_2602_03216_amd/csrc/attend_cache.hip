@@ -9,10 +9,10 @@ using namespace attend_cache_detail;
 
 namespace {
 
-template <int D, bool E4M3, int MB>
+template <int D, bool E4M3, int MB, bool ONCE>
 __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args a) {
   __shared__ __attribute__((aligned(1024))) char smem[Shape<D, E4M3, MB>::kLds];
-  few_rows<D, E4M3, MB>(a, smem, blockIdx.x);
+  few_rows<D, E4M3, MB, ONCE>(a, smem, blockIdx.x);
 }
 
 constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
@@ -156,7 +156,7 @@ constexpr int kFewRows = 64;
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
 // and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
 struct Plan {
-  bool few, many, fits;
+  bool few, many, fits, once;
   int mb, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
 };
 Plan plan_of(const CacheArgs& c) {
@@ -176,6 +176,10 @@ Plan plan_of(const CacheArgs& c) {
   // So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
   const bool small = (long long)c.n_seqs * c.Hkv * ((seen + kStep - 1) / kStep) <= 512;
   p.mb = rows <= 16 || small ? 1 : rows <= 32 || c.e4m3 ? 2 : 4;
+  // K and V that no other tile reads again pass the caches by: 64 sequences x 8192 keys, 8 KV heads, us without / with: bf16 363 / 329, 8 bits 198 / 183,
+  // d = 64 186 / 169 and 106 / 95; short ones lose little (1 x 2000 11.3 / 11.7).  Where several tiles read them it costs: four drafted tokens of 7 heads
+  // a group over 1 x 2000, 23.5 / 25.9.
+  p.once = rows <= 16 * p.mb;
   p.rows = !p.many && most * g < 16 * p.mb ? most * g : 16 * p.mb;
   p.shares = 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
@@ -211,9 +215,11 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
   const bool both = p.many && p.few && p.mb == 1;
   if (p.many && (e = launch_attend_many(a, D, E4M3, both ? p.shares : 0, st)) != hipSuccess) return e;
   if (p.few && !both) {
-    if (p.mb == 1) attend_few_rows<D, E4M3, 1><<<p.shares, 256, 0, st>>>(a);
-    else if (p.mb == 2) attend_few_rows<D, E4M3, 2><<<p.shares, 256, 0, st>>>(a);
-    else attend_few_rows<D, E4M3, 4><<<p.shares, 256, 0, st>>>(a);
+    if (p.mb == 4) attend_few_rows<D, E4M3, 4, true><<<p.shares, 256, 0, st>>>(a);
+    else if (p.mb == 2 && p.once) attend_few_rows<D, E4M3, 2, true><<<p.shares, 256, 0, st>>>(a);
+    else if (p.mb == 2) attend_few_rows<D, E4M3, 2, false><<<p.shares, 256, 0, st>>>(a);
+    else if (p.once) attend_few_rows<D, E4M3, 1, true><<<p.shares, 256, 0, st>>>(a);
+    else attend_few_rows<D, E4M3, 1, false><<<p.shares, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.few) {

@@ -35,16 +35,24 @@ struct Seq {
   __device__ __forceinline__ uint32_t span(int of) const { return of == 1 ? steps : (uint32_t)((steps + of - 1) / of) * of; }
 };
 
-__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) {
+__device__ __forceinline__ Seq sequence(const Args& a, int q0, int q_end, int kv, int rt) {
   Seq s;
-  s.q0 = a.b.first(i);
-  s.q_len = max(a.b.first(i + 1) - s.q0, 0);
-  s.kv = a.b.kv(i);
+  s.q0 = q0;
+  s.q_len = max(q_end - q0, 0);
+  s.kv = kv;
   s.rows = s.q_len * a.g;
   if (s.rows > a.few) s.rows = 0;
   s.tiles = (s.rows + rt - 1) / rt;
   s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
   s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
+  return s;
+}
+
+__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) { return sequence(a, a.b.first(i), a.b.first(i + 1), a.b.kv(i), rt); }
+__device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt) {
+  Seq s = sequence(a, one(a.b.first(i)), one(a.b.first(i + 1)), one(a.b.kv(i)), rt);
+  s.tiles = one(s.tiles);
+  s.steps = one(s.steps);
   return s;
 }
 
@@ -85,7 +93,8 @@ struct StepRegs {
 };
 
 // Share `block` of the batch, by a workgroup of 256 threads with Shape::kLds bytes of LDS at `smem`.
-template <int D, bool E4M3, int MB>
+// ONCE: no row of K and V is read twice.
+template <int D, bool E4M3, int MB, bool ONCE>
 __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned block) {
   using S = Shape<D, E4M3, MB>;
   constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
@@ -109,11 +118,13 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
   const auto sum_up = [&](uint32_t x) -> uint32_t {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    if (alone) return x;
-    __syncthreads();
-    if (lane == 0) scan[wave] = x;
-    __syncthreads();
-    return scan[0] + scan[1] + scan[2] + scan[3];
+    if (!alone) {
+      __syncthreads();
+      if (lane == 0) scan[wave] = x;
+      __syncthreads();
+      x = scan[0] + scan[1] + scan[2] + scan[3];
+    }
+    return one(x);
   };
   uint32_t mine = 0;
   over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
@@ -138,10 +149,12 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     const uint32_t o = __shfl_up(upto, m);
     if (lane >= m) upto += o;
   }
+  of = one(of);
+  share = one(share);
   uint32_t u = block * share, in_seq;
   int seq;
   if (alone) {
-    total = __shfl(upto, 63);
+    total = __builtin_amdgcn_readlane(upto, 63);
     if (u >= total) return;
     const unsigned long long behind = __builtin_amdgcn_ballot_w64(u < upto);
     if (behind == 0) return;                             // (cu_q that does not ascend)
@@ -157,6 +170,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       if (w < wave) upto += scan[w];
       total += scan[w];
     }
+    total = one(total);
     if (u >= total) return;
     uint32_t at = upto - mine;
     if (u >= at && u < upto)
@@ -169,9 +183,11 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
         at += x;
       });
     __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(place[0]);
-    in_seq = __builtin_amdgcn_readfirstlane(place[1]);
+    seq = place[0];
+    in_seq = place[1];
   }
+  seq = one(seq);
+  in_seq = one(in_seq);
   const uint32_t end = u + share < total ? u + share : total;
 
   const int lds0 = (int)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * S::kRing;
@@ -181,16 +197,19 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
   const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
 
   while (u < end) {
-    while (seq < n && sequence(a, seq, RT).tiles == 0) ++seq;
-    if (seq >= n) return;                                // (cu_q that does not ascend: the sums do not hold)
-    const Seq q = sequence(a, seq, RT);
-    const uint32_t span = q.span(of), ht = in_seq / span, h = ht / q.tiles, tile = ht - h * q.tiles;
+    Seq q;
+    for (;; ++seq) {
+      if (seq >= n) return;                              // (cu_q that does not ascend: the sums do not hold)
+      q = one_sequence(a, seq, RT);
+      if (q.tiles > 0) break;
+    }
+    const uint32_t span = one(q.span(of)), ht = one(in_seq / span), h = one(ht / q.tiles), tile = ht - h * q.tiles;
     const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
     const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
 
     // ---- the rows
     const int row0 = (int)tile * RT, pos0 = q.kv - q.q_len;
-    const int p_min = pos0 + (int)a.by_g.div(row0), p_max = pos0 + (int)a.by_g.div(min(row0 + RT, q.rows) - 1);
+    const int p_min = pos0 + one(a.by_g.div(row0)), p_max = pos0 + one(a.by_g.div(min(row0 + RT, q.rows) - 1));
     const int see_lo = a.window ? max(0, p_min - a.window + 1) : 0, see_hi = p_max + 1;     // keys that some row of the tile sees
     const int all_lo = a.window ? p_max - a.window + 1 : 0;                                 // keys all_lo .. p_min are seen by all of them
     bf16x8 qf[MB][S::NS];
@@ -224,7 +243,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
         const long long row = a.b.row(max(id, 0), (int)h, key0);
         const char* kr = a.kp + (row + lo) * RB + 16 * quarter;
 #pragma unroll
-        for (int i = 0; i < S::NK; ++i) x.k[j][i] = *(const u32x4*)(kr + 64 * i);
+        for (int i = 0; i < S::NK; ++i) x.k[j][i] = ONCE ? __builtin_nontemporal_load((const u32x4*)(kr + 64 * i)) : *(const u32x4*)(kr + 64 * i);
         if (E4M3) {
           x.ks[j] = a.ks[row + lo];
           x.vs[j] = *(const uint32_t*)(a.vs + row + 4 * quarter);
@@ -233,7 +252,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
         for (int i = 0; i < 16 / S::RPI; ++i) {
           const int r = i * S::RPI + lane / S::LPR, piece = (lane % S::LPR) ^ S::swizzle(16 * j + r);
           const bool seen = id >= 0 && key0 + r >= see_lo && key0 + r < see_hi;
-          load_row_to_lds((seen ? a.vp + (row + r) * RB : (const char*)g_zeros) + 16 * piece, lds0 + buf * (32 * RB) + (16 * j + i * S::RPI) * RB);
+          load_row_to_lds<ONCE>((seen ? a.vp + (row + r) * RB : (const char*)g_zeros) + 16 * piece, lds0 + buf * (32 * RB) + (16 * j + i * S::RPI) * RB);
         }
       }
     };
@@ -283,6 +302,15 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
             }
         }
       }
+      // (8 bits: asked for in front of the softmax; verification of 8 tokens x 32 sequences 114 -> 112 us.  In bf16 that holds too many registers: 183 -> 203.)
+      typedef __attribute__((ext_vector_type(2))) int i32x2;
+      i32x2 v8[S::ND];
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int dt = 0; dt < S::ND; ++dt)
+          v8[dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(ring + buf * (32 * RB) + (v_rd ^ (dt << 4))));
+        __builtin_amdgcn_sched_barrier(0);
+      }
       bf16x8 pf[MB];
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
@@ -315,10 +343,8 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
 #pragma unroll
       for (int dt = 0; dt < S::ND; ++dt) {
         bf16x8 vf;
-        if (E4M3) {
-          typedef __attribute__((ext_vector_type(2))) int i32x2;
-          const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(ring + buf * (32 * RB) + (v_rd ^ (dt << 4))));
-          vf = widen8((uint32_t)w[0], (uint32_t)w[1], 1.0f);
+        if constexpr (E4M3) {
+          vf = widen8((uint32_t)v8[dt][0], (uint32_t)v8[dt][1], 1.0f);
         } else {
           const char* at = ring + buf * (32 * RB) + (v_rd ^ (dt << 5));
           const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)at);
@@ -405,7 +431,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     __syncthreads();
     u += units;
     in_seq += units;
-    if (in_seq >= q.units(Hkv, of)) {
+    if (in_seq >= (uint32_t)(Hkv * q.tiles) * span) {
       ++seq;
       in_seq = 0;
     }

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
   __shared__ __attribute__((aligned(1024))) char smem[kRings > kFewLds ? kRings : kFewLds];
   if constexpr (FEW) {
     if (blockIdx.x >= grid) {
-      few_rows<D, E4M3, 1>(a, smem, blockIdx.x - grid);
+      few_rows<D, E4M3, 1, true>(a, smem, blockIdx.x - grid);
       return;
     }
   }
@@ -65,14 +65,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
 
   // ---- workgroup -> KV head, row tile, part.  id % 8 is the XCD: the row tiles of a head stay on one (or a few) of them, the last ones first.
   const unsigned xcd = blockIdx.x & 7u, at = blockIdx.x >> 3;
-  const unsigned rank = a.by_vheads.div(at), vhead = xcd * a.vheads_per_xcd + (at - rank * a.vheads_per_xcd);
+  const unsigned rank = one(a.by_vheads.div(at)), vhead = xcd * a.vheads_per_xcd + (at - rank * a.vheads_per_xcd);
   const int h = (int)(vhead >> a.split_log2);
-  const unsigned item = (rank << a.split_log2) + (vhead & ((1u << a.split_log2) - 1u)), from_last = a.by_splits.div(item);
+  const unsigned item = (rank << a.split_log2) + (vhead & ((1u << a.split_log2) - 1u)), from_last = one(a.by_splits.div(item));
   const int part = (int)(item - from_last * a.splits), slot = a.slots - 1 - (int)from_last;
   if (slot < 0) return;
-  const int seq = last_up_to(a.b.n_seqs, slot, lane, [&](int i) { return first_slot(a, i); });
+  const int seq = one(last_up_to(a.b.n_seqs, slot, lane, [&](int i) { return first_slot(a, i); }));
   if (seq < 0 || seq >= a.b.n_seqs) return;
-  const ManyTile x = many_tile(a, seq, slot - first_slot(a, seq));
+  const ManyTile x = many_tile(a, seq, slot - one(first_slot(a, seq)));
   if (!x.there || part >= x.parts) return;
   const int t0 = part * x.per, t1 = min(x.tiles, t0 + x.per);
 
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
   const int pos0 = x.kv - x.q_len, wrow0 = x.row0 + kRowsPerWave * wave, row = min(wrow0 + lo, x.rows - 1), tok = (int)a.by_g.div(row);
   const int pos = pos0 + tok;
   const bool has_rows = wrow0 < x.rows;
-  const int wp_min = pos0 + (int)a.by_g.div(min(wrow0, x.rows - 1)), wp_max = pos0 + (int)a.by_g.div(min(wrow0 + kRowsPerWave, x.rows) - 1);
+  const int wp_min = pos0 + one(a.by_g.div(min(wrow0, x.rows - 1))), wp_max = pos0 + one(a.by_g.div(min(wrow0 + kRowsPerWave, x.rows) - 1));
   const int wsee_lo = a.window ? wp_min - a.window + 1 : 0, wall_lo = a.window ? wp_max - a.window + 1 : 0, all_lo = a.window ? x.p_max - a.window + 1 : 0;
   const float c = a.c;
 
