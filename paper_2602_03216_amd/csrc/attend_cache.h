@@ -21,9 +21,9 @@ constexpr int kStep = 128;                               // keys of a step
 constexpr int kTile = 64;                                // many rows: keys of a tile
 constexpr int kPartTiles = 8;                            // ... and fewest tiles of a part
 
-// A row tile that does not end in the share it begins in (parts: 0 = there is none), parts of it, its rows.
+// A row tile of which a share has a part only: its parts (0: there is none), which one the share has, and the tile's rows.
 struct Cut {
-  int parts, q0, head, row0, rows;
+  int parts, part, q0, head, row0, rows;
 };
 
 struct Args {
@@ -40,10 +40,10 @@ struct Args {
   float c;                       // scale * log2(e)
   FastDiv by_g;
   // workspace
-  Cut* cut;                      // [shares]
+  Cut* cut;                      // [shares][2]: the one that a share begins in the midst of, the one that it ends in the midst of
   float* part_o;                 // [2 shares][rt][d]
   float* part_ml;                // [2 shares][rt][2]
-  int rt;                        // rows of a tile
+  int rt, shares;                // rows of a tile
   // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
   int few, splits, slots;
   float* many_o;                 // [slots][Hkv][splits][128][d]

@@ -17,84 +17,90 @@ __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args
 
 constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
 
-// Row tiles that a share's end cuts: the workgroup of the share that has a tile's first part, and a group of four of its rows.  The first part is
-// the second slot of its share, every later one the first slot of its share.  Wavefront r finds row r's largest max and its sum, then groups of
-// lanes take every G-th part of all four.
+// Row tiles that a share's end cuts: the shares that have a part of one deal its rows among them, four at a time.  (A workgroup for every share and group of
+// four rows, most with nothing to do, is several rounds of the chip: 8 sequences x 4000 keys, 32 rows, 14.3 us, and 5.1 so.)  The first part is the second slot
+// of its share, every later one the first slot of its share.  Wavefront r finds row r's largest max and its sum, then groups of lanes take every G-th
+// part of all four.
 template <int D>
 __global__ __launch_bounds__(256) void join_few_rows(Args a) {
   constexpr int R = 4, LPR = D / 4, G = 256 / LPR, kBatch = 2;
   __shared__ float weight[R][kMostParts];
   __shared__ float meet[G][R][D];
   __shared__ float ml[R][2];
-  const Cut c = a.cut[blockIdx.x];
-  const int parts = min(c.parts, (int)(gridDim.x - blockIdx.x));
-  if (parts == 0) return;
-  for (int r0 = R * blockIdx.y; r0 < c.rows; r0 += R * gridDim.y) {
-    const int rows = c.rows - r0;
-    const long long first = (2LL * blockIdx.x + 1) * a.rt + r0, next = (2LL * blockIdx.x + 2) * a.rt + r0;
-    const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
-    f32x4 v[kBatch][R];
-    const auto rows_from = [&](int w0) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = tid / LPR, col = 4 * (tid % LPR);
+  const Cut begins = a.cut[2 * blockIdx.x], ends = a.cut[2 * blockIdx.x + 1];
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {
+    const Cut c = side ? ends : begins;
+    if (c.parts <= 0) continue;
+    const int share = max(0, (int)blockIdx.x - max(c.part, 0)), parts = min(c.parts, a.shares - share);
+#pragma unroll 1
+    for (int r0 = R * ((int)blockIdx.x - share + parts * blockIdx.y); r0 < c.rows; r0 += R * parts * gridDim.y) {
+      const int rows = c.rows - r0;
+      const long long first = (2LL * share + 1) * a.rt + r0, next = (2LL * share + 2) * a.rt + r0;
+      const auto slot_of = [&](int w) -> long long { return w == 0 ? first : next + (long long)(w - 1) * 2 * a.rt; };
+      f32x4 v[kBatch][R];
+      const auto rows_from = [&](int w0) {
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i)
+        for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-          v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(a.part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
-    };
-    rows_from(grp);                                        // (the rows wait for nothing)
-    float m = kNone, l = 0.f;
-    if (wave < rows)
-      for (int w = lane; w < parts; w += 64) {
-        const long long slot = slot_of(w) + wave;
-        const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1], mn = fmaxf(m, mp);
+          for (int r = 0; r < R; ++r)
+            v[i][r] = w0 + i * G < parts && r < rows ? *(const f32x4*)(a.part_o + (slot_of(w0 + i * G) + r) * D + col) : f32x4{0, 0, 0, 0};
+      };
+      rows_from(grp);                                        // (the rows wait for nothing)
+      float m = kNone, l = 0.f;
+      if (wave < rows)
+        for (int w = lane; w < parts; w += 64) {
+          const long long slot = slot_of(w) + wave;
+          const float mp = a.part_ml[2 * slot], lp = a.part_ml[2 * slot + 1], mn = fmaxf(m, mp);
+          l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
+          m = mn;
+          weight[wave][w] = mp;
+        }
+#pragma unroll
+      for (int x = 1; x < 64; x <<= 1) {
+        const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
         l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
         m = mn;
-        weight[wave][w] = mp;
+      }
+      if (lane == 0) {
+        ml[wave][0] = m;
+        ml[wave][1] = l;
+      }
+      __syncthreads();
+      f32x4 o[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
+      for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - ml[r][0]);
+        rows_from(w0 + kBatch * G);
       }
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const float mp = __shfl_xor(m, x), lp = __shfl_xor(l, x), mn = fmaxf(m, mp);
-      l = l * fast_exp2(m - mn) + lp * fast_exp2(mp - mn);
-      m = mn;
-    }
-    if (lane == 0) {
-      ml[wave][0] = m;
-      ml[wave][1] = l;
-    }
-    __syncthreads();
-    f32x4 o[R];
+      for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
+      __syncthreads();
+      for (int task = tid; task < R * D / 2; task += 256) {
+        const int r = task / (D / 2), x = 2 * (task % (D / 2));
+        if (r >= rows) continue;
+        float v0 = 0.f, v1 = 0.f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) o[r] = f32x4{0, 0, 0, 0};
-    for (int w0 = grp; w0 < parts; w0 += kBatch * G) {
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-          if (w0 + i * G < parts && r < rows) o[r] += v[i][r] * fast_exp2(weight[r][w0 + i * G] - ml[r][0]);
-      rows_from(w0 + kBatch * G);
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) *(f32x4*)(&meet[grp][r][col]) = o[r];
-    __syncthreads();
-    for (int task = tid; task < R * D / 2; task += 256) {
-      const int r = task / (D / 2), x = 2 * (task % (D / 2));
-      if (r >= rows) continue;
-      float v0 = 0.f, v1 = 0.f;
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        v0 += meet[g][r][x];
-        v1 += meet[g][r][x + 1];
+        for (int g = 0; g < G; ++g) {
+          v0 += meet[g][r][x];
+          v1 += meet[g][r][x + 1];
+        }
+        const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row), tok = c.q0 + k, head = c.head * a.g + row - k * a.g;
+        const float lt = ml[r][1], inv = lt > 0.f ? 1.0f / lt : 0.f;
+        bf16x2 out;
+        out[0] = (__bf16)(v0 * inv);
+        out[1] = (__bf16)(v1 * inv);
+        *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
+        if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
       }
-      const int row = c.row0 + r0 + r, k = (int)a.by_g.div(row), tok = c.q0 + k, head = c.head * a.g + row - k * a.g;
-      const float lt = ml[r][1], inv = lt > 0.f ? 1.0f / lt : 0.f;
-      bf16x2 out;
-      out[0] = (__bf16)(v0 * inv);
-      out[1] = (__bf16)(v1 * inv);
-      *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
-      if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -196,7 +202,7 @@ struct Workspace {
 };
 Workspace workspace_of(const CacheArgs& c, const Plan& p) {
   Workspace w;
-  size_t at = align256((size_t)p.shares * sizeof(Cut));
+  size_t at = align256(2 * (size_t)p.shares * sizeof(Cut));
   auto take = [&](size_t n) { const size_t x = at; at += align256(n); return x; };
   const size_t few = 2 * (size_t)p.shares * 16 * p.mb, many = p.many && p.splits > 1 ? (size_t)p.slots * c.Hkv * p.splits * kManyRows : 0;
   w.part_ml = take(few * 2 * 4);
@@ -223,7 +229,8 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.few) {
-    join_few_rows<D><<<dim3(p.shares, (p.rows + 3) / 4), 256, 0, st>>>(a);
+    const int groups = (p.rows + 3) / 4, at_once = 1024 / p.shares;
+    join_few_rows<D><<<dim3(p.shares, groups < at_once ? groups : at_once), 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.many && p.splits > 1) {
@@ -257,7 +264,7 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.rt = 16 * p.mb; a.slots = p.slots; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.shares = p.shares; a.slots = p.slots; a.splits = p.splits;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }

@@ -142,7 +142,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       over_mine([&](int, const Seq& q) { mine += q.units(Hkv, of); });
     }
   }
-  if (tid == 0) a.cut[block].parts = 0;
+  if (tid < 2) a.cut[2 * block + tid].parts = 0;
   uint32_t upto = mine;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
@@ -393,11 +393,12 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     }
     __syncthreads();
     const bool complete = s0 == 0 && s1 == q.steps;
-    if (s0 == 0 && s1 < q.steps && tid == 0) {             // the shares that follow go on with it
-      const int more = (int)((q.steps - s1 + share - 1) / share);
-      a.cut[block] = Cut{1 + more, q.q0, (int)h, row0, min(RT, q.rows - row0)};
+    const int side = s0 == 0 ? 1 : 0;
+    if (!complete && tid == side) {
+      const uint32_t begin = u - s0, first = begin / share;
+      a.cut[2 * block + side] = Cut{(int)((begin + q.steps - 1) / share - first) + 1, (int)(block - first), q.q0, (int)h, row0, min(RT, q.rows - row0)};
     }
-    const long long slot = 2LL * block + (s0 == 0 ? 1 : 0);
+    const long long slot = 2LL * block + side;
     for (int task = tid; task < RT * (D / 8); task += 256) {
       const int r = task / (D / 8), col = 8 * (task % (D / 8));
       if (row0 + r >= q.rows) continue;
