@@ -177,11 +177,11 @@ Plan plan_of(const CacheArgs& c) {
   p.fits = !p.few || steps(p.many ? rows_few : rows_all) < 4.0e9;
   const int rows = p.many ? g : most * g;                // (beside prompts: single tokens, most likely)
   // Rows of a tile.  Larger tiles read K and V fewer times, smaller ones start and end sooner and are more of them.  28 / 4 heads, us with tiles of
-  // 16 / 32 / 64 rows: 32 sequences x 8000 keys, 3 new tokens (21 rows) bf16 160 / 109 / 114, 8 bits 87 / 60 / 96; 8 new tokens (56 rows) 298 / 166 / 122
-  // and 155 / 99 / 103; 200 x 500, 56 rows, 131 / 84 / 76 and 83 / 68 / 75; 2 x 300, 56 rows, 11.5 / 13.3 / 17.0 and 11.1 / 13.3 / 16.8; 1 x 2000 15.1 / 16.7 / 19.9.
-  // So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
+  // 16 / 32 / 64 rows: 32 sequences x 8000 keys, 3 new tokens (21 rows) bf16 156 / 96 / 99, 8 bits 87 / 58 / 90; 8 new tokens (56 rows) 292 / 163 / 103 and
+  // 153 / 94 / 94 (d = 64: 149 / 87 / 59 and 91 / 64 / 53); 200 x 500, 56 rows, 139 / 92 / 87 and 87 / 69 / 80; 2 x 300, 56 rows, 11.6 / 15.0 / 18.1 and
+  // 11.0 / 13.9 / 17.3; 1 x 2000 12.6 / 14.0 / 17.5.  So 16 rows where the steps of the whole capacity run at once whatever the lengths are.
   const bool small = (long long)c.n_seqs * c.Hkv * ((seen + kStep - 1) / kStep) <= 512;
-  p.mb = rows <= 16 || small ? 1 : rows <= 32 || c.e4m3 ? 2 : 4;
+  p.mb = rows <= 16 || small ? 1 : rows <= 32 || (c.e4m3 && c.d == 128) ? 2 : 4;
   // K and V that no other tile reads again pass the caches by: 64 sequences x 8192 keys, 8 KV heads, us without / with: bf16 363 / 329, 8 bits 198 / 183,
   // d = 64 186 / 169 and 106 / 95; short ones lose little (1 x 2000 11.3 / 11.7).  Where several tiles read them it costs: four drafted tokens of 7 heads
   // a group over 1 x 2000, 23.5 / 25.9.
@@ -222,9 +222,12 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
   if (p.many && (e = launch_attend_many(a, D, E4M3, both ? p.shares : 0, st)) != hipSuccess) return e;
   if (p.few && !both) {
     if (p.mb == 4) attend_few_rows<D, E4M3, 4, true><<<p.shares, 256, 0, st>>>(a);
-    else if (p.mb == 2 && p.once) attend_few_rows<D, E4M3, 2, true><<<p.shares, 256, 0, st>>>(a);
-    else if (p.mb == 2) attend_few_rows<D, E4M3, 2, false><<<p.shares, 256, 0, st>>>(a);
-    else if (p.once) attend_few_rows<D, E4M3, 1, true><<<p.shares, 256, 0, st>>>(a);
+    else if (p.mb == 2) {
+      bool once = true;
+      if constexpr (E4M3 && D == 128) once = p.once;     // (the only ones whose 33 to 64 rows are not one tile)
+      if (once) attend_few_rows<D, E4M3, 2, true><<<p.shares, 256, 0, st>>>(a);
+      else if constexpr (E4M3 && D == 128) attend_few_rows<D, E4M3, 2, false><<<p.shares, 256, 0, st>>>(a);
+    } else if (p.once) attend_few_rows<D, E4M3, 1, true><<<p.shares, 256, 0, st>>>(a);
     else attend_few_rows<D, E4M3, 1, false><<<p.shares, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

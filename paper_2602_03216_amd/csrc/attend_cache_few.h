@@ -57,8 +57,8 @@ __device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt) {
 }
 
 // Shares per CU, all of which run at once.  What they have in flight together is what the memory rate comes from: the rows of d = 64 in 8 bits
-// are short and take four (300 sequences x 1000 keys, 8 KV heads: 97 -> 81 us, 6 x 131072 158 -> 151); with longer rows two have enough in
-// flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 195 us with two, 207 with three; bf16, d = 64: 189 with two, 195 with four).
+// are short and take four (300 sequences x 1000 keys, 8 KV heads: 83 us with two, 70 with four, 6 x 131072 153 and 138); with longer rows two have enough
+// in flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 176 us with two, 189 with three; bf16, d = 64: 170 with two, 176 with four).
 constexpr int per_cu(int d, bool e4m3, int mb) { return mb == 4 && d == 128 ? 1 : mb == 1 && d == 64 && e4m3 ? 4 : 2; }
 
 template <int D, bool E4M3, int MB>

@@ -156,6 +156,16 @@ def test_random_batches(tsa, seed, e4m3, d, page):
     b.check(*b.run(tsa))
 
 
+@pytest.mark.parametrize("window", [0, 900])
+@pytest.mark.parametrize("new", [(3, 1, 2, 3, 3), (5, 2, 5, 4, 1), (8, 9, 7, 1, 9)])
+@pytest.mark.parametrize("e4m3,d", [(0, 128), (1, 128), (0, 64), (1, 64)])
+def test_row_tiles_of_every_height(tsa, e4m3, d, new, window):
+    """Seven query heads a group, up to 21, 35 and 63 rows a sequence, over caches that are long enough to be dealt by more than one share a head."""
+    kv = [4500, 17, 130, 2900, 4001]
+    b = Batch(50 + d + e4m3, list(new), kv, 28, 4, d, 16, e4m3=e4m3, window=window, gone=[(0, 7), (0, 8), (3, 100), (4, 250)])
+    b.check(*b.run(tsa))
+
+
 @pytest.mark.parametrize("name", ["one_token", "mixed", "window", "more_new_than_cached"])
 def test_what_the_caller_knows_does_not_change_what_is_computed(tsa, name):
     """Any max_q, another workspace: right all the same; the same call twice: the same bits."""
