@@ -208,3 +208,21 @@ def test_captured(tsa):
         step()
         assert all(torch.equal(a, b) for a, b in zip(got, (K, V, kp, ks)))
         assert K[1, :, 4 + 18 * k:].abs().max() == 0 and K[1, :, :4 + 18 * k].abs().sum() > 0
+
+
+def test_values_that_are_no_numbers(tsa):
+    """8 bits: they become NaN, and the row's exponent is the largest; the rows beside them are as without them."""
+    K = torch.randn(5, 2, 64, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).to(gu.DEV)
+    bad = K.clone()
+    bad[0, 0, 3], bad[1, 0, 4], bad[2, 1, 5] = float("inf"), float("nan"), -float("inf")
+    desc = tsa.make_cache_desc(1, 5, 2, 2, 64, 16, 1, 1, tsa.TSA_CACHE_E4M3)
+    pools = []
+    for x in (K, bad):
+        kp, ks = torch.zeros(1, 2, 16, 64, dtype=torch.uint8, device=gu.DEV), torch.zeros(1, 2, 16, dtype=torch.uint8, device=gu.DEV)
+        tsa.tsa_cache_write(desc, x, x, _ints([0, 5]), _ints([5]), _ints([[0]]), kp, kp.clone(), ks, ks.clone())
+        pools.append((kp[0].cpu(), ks[0].cpu()))
+    (kp, ks), (kp2, ks2) = pools
+    for t, h, i in ((0, 0, 3), (1, 0, 4), (2, 1, 5)):
+        assert ks2[h, t] == 247 and kp2[h, t, i] & 0x7f == 0x7f and (kp2[h, t] & 0x7f == 0x7f).sum() == 1
+        kp2[h, t], ks2[h, t] = kp[h, t], ks[h, t]
+    assert torch.equal(kp, kp2) and torch.equal(ks, ks2)
