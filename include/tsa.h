@@ -363,7 +363,8 @@ typedef struct tsa_cache_desc {
 } tsa_cache_desc;
 
 /* Writes the new rows of K and V [n_tokens,Hkv,d] bf16 into their pages: as they are, or in 8 bits as e4m3(x 2^-e), nearest even, with
- * the smallest e >= -126 for which the largest magnitude of the row fits (max |x| <= 448 * 2^e; e = 0 for a row of zeros). */
+ * the smallest e >= -126 for which the largest magnitude of the row fits (max |x| <= 448 * 2^e; e = 0 for a row of zeros).  In 8 bits an
+ * infinity or a NaN becomes a NaN and the row's largest magnitude; what rounds up to 2^128 reads back as infinity. */
 int tsa_cache_write(const tsa_cache_desc* desc, const void* K, const void* V, const int32_t* cu_q, const int32_t* kv_len,
                     const int32_t* page_table, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream);
 
@@ -376,7 +377,8 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
  * p = kv_len[i] - (cu_q[i + 1] - t) sees the keys at positions <= p of its sequence (within the window, if the descriptor has one) that are
  * on pages that are there.  Single tokens, drafted tokens, pieces of prompts and whole prompts, mixed as they come.
  *   Q [n_tokens,Hq,d] bf16;  O [n_tokens,Hq,d] bf16 out;  lse [n_tokens,Hq] fp32 out or NULL (natural-log sum-exp of the scaled logits)
- *   A token that sees no key gets zeros and -infinity.
+ *   A token that sees no key gets zeros and -infinity.  O overlaps no input.  A NaN or an infinity in a row of V may reach tokens of the call
+ *   that do not see it; in K it reaches those that do.
  *   ws: tsa_attend_cache_workspace_bytes(desc) bytes; its contents need not be kept between calls
  * Arithmetic as in tsa_attend; 8-bit rows are widened exactly. The same inputs give the same bits. */
 size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc);

@@ -720,6 +720,7 @@ int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pa
   const size_t need = tsa::attend_cache_ws_bytes(c);
   if (need == 0) return fail(TSA_ERR_UNSUPPORTED, "n_seqs * Hkv * max_pages * page_size is too large: keys are counted in 2^32 steps of 128");
   if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+  if (O == Q) return fail(TSA_ERR_ARG, "O is Q");
   c.cu_q = cu_q;
   return hip_status(tsa::launch_attend_cache(c, Q, O, lse, ws, (hipStream_t)stream), "tsa_attend_cache");
 }

@@ -101,7 +101,7 @@ __device__ __forceinline__ ManyTile many_tile(const Args& a, int seq, int tile) 
   x.kv = one(a.b.kv(seq));
   x.rows = x.q_len * a.g;
   x.row0 = tile * kManyRows;
-  x.there = x.rows > a.few && x.row0 < x.rows;
+  x.there = tile >= 0 && x.rows > a.few && x.row0 < x.rows;      // (tile < 0: cu_q that does not ascend)
   const int pos0 = x.kv - x.q_len;
   x.p_min = pos0 + one(a.by_g.div(max(0, min(x.row0, x.rows - 1))));
   x.p_max = pos0 + one(a.by_g.div(max(0, min(x.row0 + kManyRows, x.rows) - 1)));

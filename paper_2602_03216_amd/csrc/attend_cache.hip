@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void join_few_rows(Args a) {
         out[0] = (__bf16)(v0 * inv);
         out[1] = (__bf16)(v1 * inv);
         *(bf16x2*)(a.O + tok * a.o_t + head * a.o_h + x) = out;
-        if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt > 0.f ? (ml[r][0] + log2f(lt)) * kLn2 : -INFINITY;
+        if (a.lse && x == 0) a.lse[(long long)tok * a.Hq + head] = lt == 0.f ? -INFINITY : (ml[r][0] + log2f(lt)) * kLn2;
       }
       __syncthreads();
     }
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256) void join_many_rows(Args a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = (__bf16)(o[i] * inv);
     *(bf16x4*)(a.O + tok * a.o_t + head * a.o_h + col) = out;
-    if (a.lse && col == 0) a.lse[(long long)tok * a.Hq + head] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    if (a.lse && col == 0) a.lse[(long long)tok * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
 }
 

@@ -204,6 +204,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       if (q.tiles > 0) break;
     }
     const uint32_t span = one(q.span(of)), ht = one(in_seq / span), h = one(ht / q.tiles), tile = ht - h * q.tiles;
+    if (h >= (uint32_t)Hkv) return;                        // (the same)
     const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
     const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
 
@@ -418,7 +419,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[i] = (__bf16)(v[i >> 2][i & 3] * inv);
         *(bf16x8*)(a.O + (q.q0 + tok) * a.o_t + head * a.o_h + col) = out;
-        if (a.lse && col == 0) a.lse[(long long)(q.q0 + tok) * a.Hq + head] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+        if (a.lse && col == 0) a.lse[(long long)(q.q0 + tok) * a.Hq + head] = lt == 0.f ? -INFINITY : (mt + log2f(lt)) * kLn2;
       } else {
         float* dst = a.part_o + (slot * RT + r) * D + col;
         *(f32x4*)dst = v[0];

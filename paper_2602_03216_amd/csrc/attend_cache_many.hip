@@ -436,7 +436,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
     }
   }
   if (a.lse && hi == 0 && wrow0 + lo < x.rows)
-    a.lse[(long long)(x.q0 + tok) * a.Hq + h * a.g + row - tok * a.g] = lt > 0.f ? (m[0] + log2f(lt)) * kLn2 : -INFINITY;
+    a.lse[(long long)(x.q0 + tok) * a.Hq + h * a.g + row - tok * a.g] = lt == 0.f ? -INFINITY : (m[0] + log2f(lt)) * kLn2;
 }
 
 }  // namespace

@@ -107,5 +107,6 @@ def test_attend_refused():
     assert need > 0 and _attend(d, n=need - 1) == small and _attend(d, ws=None) == small and _attend(d, ws=ctypes.c_void_p(0x1080)) == small
     assert _attend(_desc(n_tokens=1 << 22, Hq=1024, Hkv=1)) == tsa.TSA_ERR_UNSUPPORTED
     assert _attend(_desc(n_tokens=0), Q=None, O=None, ws=None, n=0) == tsa.TSA_OK
+    assert _attend(d) == arg and "O is Q" in tsa.tsa_last_error()
     with pytest.raises(tsa.TsaError):
         tsa.alloc_attend_cache_workspace(_desc(d=80))

@@ -275,3 +275,37 @@ def test_lengths_that_do_not_fit(tsa):
             if kv[i] == b.kv[i] and cu[i + 1] == b.cu[i + 1]:
                 cut = slice(b.cu[i], b.cu[i + 1])
                 assert (O[cut].double() - want[cut].double()).abs().max() <= 2.0 ** -6      # (another partition of the keys: other roundings)
+
+
+@pytest.mark.parametrize("n", [3, 70])
+def test_first_rows_that_do_not_ascend(tsa, n):
+    """Whatever cu_q holds, every access stays inside the tensors; the call after it is right."""
+    new = [1, 3, 200] + [2] * (n - 3)
+    b = Batch(7300 + n, new, [k + 60 for k in new], 8, 2, 128, 16)
+    guard = 64
+    rows = torch.full((b.T + 2 * guard, b.Hq, b.d), 7.0, dtype=torch.bfloat16, device=gu.DEV)
+    O = rows[guard:guard + b.T]
+    r = np.random.Generator(np.random.PCG64(7400 + n))
+    for max_q in (0, 1, 200):
+        desc = b.desc(tsa, max_q=max_q)
+        ws = tsa.alloc_attend_cache_workspace(desc)
+        flat = np.zeros(n + 1, dtype=np.int64)
+        for cu in (b.cu[::-1].copy(), np.where(np.arange(n + 1) % 2, b.T, 0), np.where(np.arange(n + 1) % 2, 0, b.T), flat, flat - 5, flat + b.T,
+                   r.integers(-(1 << 31), 1 << 31, n + 1), r.integers(0, b.T + 1, n + 1), np.concatenate([[b.T], b.cu[:-1]])):
+            tsa.tsa_attend_cache(desc, gu.to_dev(b.q), *b.pools, ints(cu), ints(b.kv), ints(b.tab), O, ws)
+            assert (rows[:guard] == 7).all() and (rows[guard + b.T:] == 7).all()
+        b.check(*b.run(tsa, ws=ws, max_q=max_q))
+
+
+@pytest.mark.parametrize("name", ["seven_heads", "mixed", "long"])
+def test_a_query_that_is_not_a_number(tsa, name):
+    """Its row says so in O and in lse; the others are right."""
+    b = Batch(7500, **CASES[name])
+    t, h = b.T // 2, b.Hq - 1
+    O, lse = b.run(tsa)
+    Q = gu.to_dev(b.q)
+    Q[t, h, 5] = float("nan")
+    got, got_lse = b.run(tsa, Q=Q)
+    assert got[t, h].isnan().all() and got_lse[t, h].isnan()
+    got[t, h], got_lse[t, h] = O[t, h], lse[t, h]
+    b.check(got, got_lse)
