@@ -43,7 +43,7 @@ struct Args {
   Cut* cut;                      // [shares][2]: the one that a share begins in the midst of, the one that it ends in the midst of
   float* part_o;                 // [2 shares][rt][d]
   float* part_ml;                // [2 shares][rt][2]
-  int rt, shares;                // rows of a tile
+  int rt, shares, whole;         // rows of a tile; whole tiles of a sequence that run side by side
   // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
   int few, splits, slots;
   float* many_o;                 // [slots][Hkv][splits][128][d]

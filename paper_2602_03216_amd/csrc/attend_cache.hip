@@ -12,7 +12,13 @@ namespace {
 template <int D, bool E4M3, int MB, bool ONCE>
 __global__ __launch_bounds__(256, per_cu(D, E4M3, MB)) void attend_few_rows(Args a) {
   __shared__ __attribute__((aligned(1024))) char smem[Shape<D, E4M3, MB>::kLds];
-  few_rows<D, E4M3, MB, ONCE>(a, smem, blockIdx.x);
+  few_rows<D, E4M3, MB, ONCE, false>(a, smem, blockIdx.x);
+}
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(512, 1) void attend_whole_tiles(Args a) {
+  __shared__ __attribute__((aligned(1024))) char smem[Shape<D, E4M3, 1, 8>::kLds];
+  few_rows<D, E4M3, 1, false, true>(a, smem, blockIdx.x);
 }
 
 constexpr int kMostParts = 1024;                         // shares, or parts of a row tile's keys: no row has more
@@ -162,8 +168,8 @@ constexpr int kFewRows = 64;
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
 // and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
 struct Plan {
-  bool few, many, fits, once;
-  int mb, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
+  bool few, many, fits, once, whole;
+  int mb, tiles, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
 };
 Plan plan_of(const CacheArgs& c) {
   const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
@@ -187,7 +193,15 @@ Plan plan_of(const CacheArgs& c) {
   // a group over 1 x 2000, 23.5 / 25.9.
   p.once = rows <= 16 * p.mb;
   p.rows = !p.many && most * g < 16 * p.mb ? most * g : 16 * p.mb;
-  p.shares = 256 * per_cu(c.d, c.e4m3, p.mb);
+  // Short contexts of few sequences: whole row tiles by workgroups of twice the wavefronts, at most one per CU, without parts and so without a second
+  // launch (3 us of the host's time beside what follows).  us in shares / whole, 8 KV heads, one token: 1 sequence x 500 keys bf16 10.8 / 9.3, 8 bits 10.3 /
+  // 7.8, d = 64 9.6 / 6.0 and 9.5 / 5.7; x 1000 11.2 / 13.9, 10.8 / 11.7, 9.8 / 9.0, 9.6 / 7.6; 32 sequences x 1000 30.4 / 26.7, 22.5 / 17.6, 20.2 / 15.8,
+  // 17.4 / 12.2; x 2000 49.7 / 48.8, 32.6 / 29.3, 29.8 / 26.5, 22.9 / 18.5; 64 x 1000 48.0 / 51.3, 31.2 / 34.2, 27.7 / 29.6, 22.8 / 22.1.  Few tiles wait for every
+  // step's latency, so many keys are better dealt out; rows of 128 bytes or less, or 128 tiles and more, bear twice as many.
+  p.tiles = (most * g + 15) / 16;
+  const long long whole_tiles = (long long)c.n_seqs * c.Hkv * p.tiles;
+  p.whole = !p.many && p.mb == 1 && whole_tiles <= 256 && seen <= (512 << ((c.d == 64 || c.e4m3) + (whole_tiles >= 128)));
+  p.shares = p.whole ? 1 : 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
   const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
   const long long most_parts = cap / (kTile * kPartTiles);
@@ -220,6 +234,10 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
   // with tiles of 16 rows the shares run in the same launch as the rows of many, behind them: in its tail
   const bool both = p.many && p.few && p.mb == 1;
   if (p.many && (e = launch_attend_many(a, D, E4M3, both ? p.shares : 0, st)) != hipSuccess) return e;
+  if (p.whole) {
+    attend_whole_tiles<D, E4M3><<<a.b.n_seqs * p.tiles * a.b.Hkv, 512, 0, st>>>(a);
+    return hipGetLastError();
+  }
   if (p.few && !both) {
     if (p.mb == 4) attend_few_rows<D, E4M3, 4, true><<<p.shares, 256, 0, st>>>(a);
     else if (p.mb == 2) {
@@ -267,7 +285,7 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.rt = 16 * p.mb; a.shares = p.shares; a.slots = p.slots; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.shares = p.shares; a.whole = p.tiles; a.slots = p.slots; a.splits = p.splits;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }

@@ -8,7 +8,7 @@
 // fills the chip.  The work of the whole batch, counted in steps of 128 keys of one (sequence, KV head, tile of 16 rows), is cut into
 // equal shares, one per workgroup; lengths are known on the device only, so every workgroup sums them up itself and finds its
 // place.  A share that covers only a part of a row tile's keys leaves its running max, sum and output in the workspace, and a second launch
-// joins them; whole ones are written at once.
+// joins them; whole ones are written at once.  Where contexts are short and few, a workgroup takes a whole tile instead (WHOLE).
 //   A wavefront takes 32 keys of a step, with a softmax of its own; the four meet at the end of a segment.  S^T = K Q^T on
 // v_mfma_f32_16x16x32_bf16: rows = keys, columns = the tile's rows, so a lane keeps one row's max and sum.  K goes from memory straight
 // into the registers of that product (a lane's 16 bytes are its operand).  O^T = V^T P^T takes the probabilities as the lane holds them: its
@@ -35,7 +35,7 @@ struct Seq {
   __device__ __forceinline__ uint32_t span(int of) const { return of == 1 ? steps : (uint32_t)((steps + of - 1) / of) * of; }
 };
 
-__device__ __forceinline__ Seq sequence(const Args& a, int q0, int q_end, int kv, int rt) {
+__device__ __forceinline__ Seq sequence(const Args& a, int q0, int q_end, int kv, int rt, int step) {
   Seq s;
   s.q0 = q0;
   s.q_len = max(q_end - q0, 0);
@@ -44,13 +44,13 @@ __device__ __forceinline__ Seq sequence(const Args& a, int q0, int q_end, int kv
   if (s.rows > a.few) s.rows = 0;
   s.tiles = (s.rows + rt - 1) / rt;
   s.first = a.window ? max(0, s.kv - s.q_len - a.window + 1) & ~15 : 0;
-  s.steps = max(1, (s.kv - s.first + kStep - 1) / kStep);
+  s.steps = max(1, (s.kv - s.first + step - 1) / step);
   return s;
 }
 
-__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) { return sequence(a, a.b.first(i), a.b.first(i + 1), a.b.kv(i), rt); }
-__device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt) {
-  Seq s = sequence(a, one(a.b.first(i)), one(a.b.first(i + 1)), one(a.b.kv(i)), rt);
+__device__ __forceinline__ Seq sequence(const Args& a, int i, int rt) { return sequence(a, a.b.first(i), a.b.first(i + 1), a.b.kv(i), rt, kStep); }
+__device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt, int step) {
+  Seq s = sequence(a, one(a.b.first(i)), one(a.b.first(i + 1)), one(a.b.kv(i)), rt, step);
   s.tiles = one(s.tiles);
   s.steps = one(s.steps);
   return s;
@@ -61,7 +61,7 @@ __device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt) {
 // in flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 176 us with two, 189 with three; bf16, d = 64: 170 with two, 176 with four).
 constexpr int per_cu(int d, bool e4m3, int mb) { return mb == 4 && d == 128 ? 1 : mb == 1 && d == 64 && e4m3 ? 4 : 2; }
 
-template <int D, bool E4M3, int MB>
+template <int D, bool E4M3, int MB, int NW = 4>
 struct Shape {
   static constexpr int RT = 16 * MB;                     // rows of a tile
   static constexpr int kPerCU = per_cu(D, E4M3, MB), kShares = 256 * kPerCU;
@@ -71,10 +71,10 @@ struct Shape {
   static constexpr int NS = D / 32, ND = D / 16;         // k-steps of the first product, column tiles of the second
   static constexpr int kRing = 2 * 32 * RB;              // LDS bytes of a wavefront: two steps of V
   static constexpr int OS = D + 4;                       // floats between rows where the wavefronts meet
-  static constexpr int kMerge = 4 * RT * OS * 4;
-  static constexpr int kTiles = 4 * kRing > kMerge ? 4 * kRing : kMerge;
+  static constexpr int kMerge = NW * RT * OS * 4;
+  static constexpr int kTiles = NW * kRing > kMerge ? NW * kRing : kMerge;
   struct Tail {
-    float ml[4][RT][2];                                  // where the wavefronts meet: max and sum of every row
+    float ml[NW][RT][2];                                  // where the wavefronts meet: max and sum of every row
     uint32_t scan[4], place[2];
   };
   static constexpr int kLds = kTiles + (int)sizeof(Tail);
@@ -92,11 +92,12 @@ struct StepRegs {
   uint32_t ks[2], vs[2];
 };
 
-// Share `block` of the batch, by a workgroup of 256 threads with Shape::kLds bytes of LDS at `smem`.
-// ONCE: no row of K and V is read twice.
-template <int D, bool E4M3, int MB, bool ONCE>
+// Share `block` of the batch, by a workgroup of 256 threads with Shape::kLds bytes of LDS at `smem`.  ONCE: no row of K and V is read twice.
+// WHOLE: by one of 512 threads that takes whole row tiles, in steps of 256 keys; `block` counts KV heads, then a.whole tiles of a sequence, then sequences.
+template <int D, bool E4M3, int MB, bool ONCE, bool WHOLE>
 __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned block) {
-  using S = Shape<D, E4M3, MB>;
+  constexpr int NW = WHOLE ? 8 : 4, kKeys = 32 * NW, kBlocks = 2 * NW, kChunkLog2 = WHOLE ? 2 : 3;      // keys of a step, 16 of them each, steps of 64 such
+  using S = Shape<D, E4M3, MB, NW>;
   constexpr int RT = S::RT, RB = S::RB, kShares = S::kShares;
   auto& tail = *(typename S::Tail*)(smem + S::kTiles);
   auto& ml = tail.ml;
@@ -104,91 +105,99 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
   auto& place = tail.place;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, quarter = lane >> 4;
   const int n = a.b.n_seqs, Hkv = a.b.Hkv;
-
-  // ---- the share: thread t counts sequences t * per .. of the batch.  Where a few steps more than an equal share let no share go over the end of
-  // a row tile, the tiles are counted as multiples of such a share: another tile in a share costs a meeting of the wavefronts and a start, which is
-  // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 28).
-  // (Up to 64 sequences every wavefront does it for itself, a sequence per lane, without a barrier.)
-  const bool alone = n <= 64;
-  const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
-  const Seq own = sequence(a, min(i0, n - 1), RT);
-  const auto over_mine = [&](auto&& f) {
-    for (int i = i0; i < i1; ++i) f(i, per == 1 ? own : sequence(a, i, RT));
-  };
-  const auto sum_up = [&](uint32_t x) -> uint32_t {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    if (!alone) {
-      __syncthreads();
-      if (lane == 0) scan[wave] = x;
-      __syncthreads();
-      x = scan[0] + scan[1] + scan[2] + scan[3];
-    }
-    return one(x);
-  };
-  uint32_t mine = 0;
-  over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
-  uint32_t total = sum_up(mine), share = (total + kShares - 1) / kShares;
-  int of = 1;
-  if (share > 1) {
-    for (int k = 0; k < 4 && of == 1; ++k) {
-      uint32_t parts = 0;                                // shares that whole ones of share + k steps make
-      over_mine([&](int, const Seq& q) { parts += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k - 1) / (share + k)); });
-      if (sum_up(parts) <= (uint32_t)kShares) of = (int)share + k;
-    }
-    if (of > 1) {
-      share = of;
-      mine = 0;
-      over_mine([&](int, const Seq& q) { mine += q.units(Hkv, of); });
-    }
-  }
-  if (tid < 2) a.cut[2 * block + tid].parts = 0;
-  uint32_t upto = mine;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint32_t o = __shfl_up(upto, m);
-    if (lane >= m) upto += o;
-  }
-  of = one(of);
-  share = one(share);
-  uint32_t u = block * share, in_seq;
-  int seq;
-  if (alone) {
-    total = __builtin_amdgcn_readlane(upto, 63);
-    if (u >= total) return;
-    const unsigned long long behind = __builtin_amdgcn_ballot_w64(u < upto);
-    if (behind == 0) return;                             // (cu_q that does not ascend)
-    seq = __ffsll((long long)behind) - 1;
-    in_seq = u - __builtin_amdgcn_readlane(upto - mine, seq);
+  uint32_t share = 0, u = 0, end = 0, in_seq = 0;
+  int of = 1, seq = 0, whole_h = 0, whole_tile = 0;
+  if constexpr (WHOLE) {
+    const int rest = one((int)(block / (unsigned)Hkv));
+    whole_h = (int)block - rest * Hkv;
+    seq = one(rest / a.whole);
+    whole_tile = rest - seq * a.whole;
+    if (seq >= n) return;
   } else {
-    __syncthreads();
-    if (lane == 63) scan[wave] = upto;
-    if (tid == 0) place[0] = n;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) upto += scan[w];
-      total += scan[w];
+    // ---- the share: thread t counts sequences t * per .. of the batch.  Where a few steps more than an equal share let no share go over the end of
+    // a row tile, the tiles are counted as multiples of such a share: another tile in a share costs a meeting of the wavefronts and a start, which is
+    // about as long as three steps (9 sequences x 4096 keys, 4 KV heads, two row tiles, 8 bits: equal shares of 4.5 steps 34 us, whole ones of 5 28).
+    // (Up to 64 sequences every wavefront does it for itself, a sequence per lane, without a barrier.)
+    const bool alone = n <= 64;
+    const int per = (n + 255) / 256, who = alone ? lane : tid, i0 = who * per, i1 = min(n, i0 + per);
+    const Seq own = sequence(a, min(i0, n - 1), RT);
+    const auto over_mine = [&](auto&& f) {
+      for (int i = i0; i < i1; ++i) f(i, per == 1 ? own : sequence(a, i, RT));
+    };
+    const auto sum_up = [&](uint32_t x) -> uint32_t {
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+      if (!alone) {
+        __syncthreads();
+        if (lane == 0) scan[wave] = x;
+        __syncthreads();
+        x = scan[0] + scan[1] + scan[2] + scan[3];
+      }
+      return one(x);
+    };
+    uint32_t mine = 0;
+    over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
+    uint32_t total = sum_up(mine);
+    share = (total + kShares - 1) / kShares;
+    if (share > 1) {
+      for (int k = 0; k < 4 && of == 1; ++k) {
+        uint32_t parts = 0;                                // shares that whole ones of share + k steps make
+        over_mine([&](int, const Seq& q) { parts += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k - 1) / (share + k)); });
+        if (sum_up(parts) <= (uint32_t)kShares) of = (int)share + k;
+      }
+      if (of > 1) {
+        share = of;
+        mine = 0;
+        over_mine([&](int, const Seq& q) { mine += q.units(Hkv, of); });
+      }
     }
-    total = one(total);
-    if (u >= total) return;
-    uint32_t at = upto - mine;
-    if (u >= at && u < upto)
-      over_mine([&](int i, const Seq& q) {
-        const uint32_t x = q.units(Hkv, of);
-        if (u >= at && u < at + x) {
-          place[0] = i;
-          place[1] = u - at;
-        }
-        at += x;
-      });
-    __syncthreads();
-    seq = place[0];
-    in_seq = place[1];
+    if (tid < 2) a.cut[2 * block + tid].parts = 0;
+    uint32_t upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const uint32_t o = __shfl_up(upto, m);
+      if (lane >= m) upto += o;
+    }
+    of = one(of);
+    share = one(share);
+    u = block * share;
+    if (alone) {
+      total = __builtin_amdgcn_readlane(upto, 63);
+      if (u >= total) return;
+      const unsigned long long behind = __builtin_amdgcn_ballot_w64(u < upto);
+      if (behind == 0) return;                             // (cu_q that does not ascend)
+      seq = __ffsll((long long)behind) - 1;
+      in_seq = u - __builtin_amdgcn_readlane(upto - mine, seq);
+    } else {
+      __syncthreads();
+      if (lane == 63) scan[wave] = upto;
+      if (tid == 0) place[0] = n;
+      __syncthreads();
+      total = 0;
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) upto += scan[w];
+        total += scan[w];
+      }
+      total = one(total);
+      if (u >= total) return;
+      uint32_t at = upto - mine;
+      if (u >= at && u < upto)
+        over_mine([&](int i, const Seq& q) {
+          const uint32_t x = q.units(Hkv, of);
+          if (u >= at && u < at + x) {
+            place[0] = i;
+            place[1] = u - at;
+          }
+          at += x;
+        });
+      __syncthreads();
+      seq = place[0];
+      in_seq = place[1];
+    }
+    seq = one(seq);
+    in_seq = one(in_seq);
+    end = u + share < total ? u + share : total;
   }
-  seq = one(seq);
-  in_seq = one(in_seq);
-  const uint32_t end = u + share < total ? u + share : total;
 
   const int lds0 = (int)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * S::kRing;
   char* const ring = smem + wave * S::kRing;
@@ -196,20 +205,33 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
   const int v_row = E4M3 ? 4 * quarter + ((lo >> 1) & 3) + ((lo >> 3) << 4) : 4 * quarter + (lo >> 2);
   const int v_rd = v_row * RB + (E4M3 ? (S::swizzle(v_row) << 4) + 8 * (lo & 1) : ((S::swizzle(v_row) ^ ((lo >> 1) & 1)) << 4) + 8 * (lo & 1));
 
-  while (u < end) {
-    Seq q;
-    for (;; ++seq) {
-      if (seq >= n) return;                              // (cu_q that does not ascend: the sums do not hold)
-      q = one_sequence(a, seq, RT);
-      if (q.tiles > 0) break;
+  Seq q;
+  if constexpr (WHOLE) q = one_sequence(a, seq, RT, kKeys);
+  while (WHOLE || u < end) {
+    uint32_t span = 0, units = 0;
+    int h = whole_h, tile = whole_tile, s0 = 0, s1 = 0;
+    if constexpr (WHOLE) {
+      if (tile >= q.tiles) return;
+      s1 = q.steps;
+    } else {
+      for (;; ++seq) {
+        if (seq >= n) return;                              // (cu_q that does not ascend: the sums do not hold)
+        q = one_sequence(a, seq, RT, kKeys);
+        if (q.tiles > 0) break;
+      }
+      span = one(q.span(of));
+      const uint32_t ht = one(in_seq / span);
+      h = one(ht / q.tiles);
+      if (h >= Hkv) return;                                // (the same)
+      tile = ht - h * q.tiles;
+      const uint32_t in_tile = in_seq - ht * span;
+      units = min(end - u, span - in_tile);
+      s0 = (int)in_tile;
+      s1 = min((int)(in_tile + units), q.steps);
     }
-    const uint32_t span = one(q.span(of)), ht = one(in_seq / span), h = one(ht / q.tiles), tile = ht - h * q.tiles;
-    if (h >= (uint32_t)Hkv) return;                        // (the same)
-    const uint32_t in_tile = in_seq - ht * span, units = min(end - u, span - in_tile);
-    const int s0 = (int)in_tile, s1 = min((int)(in_tile + units), q.steps);
 
     // ---- the rows
-    const int row0 = (int)tile * RT, pos0 = q.kv - q.q_len;
+    const int row0 = tile * RT, pos0 = q.kv - q.q_len;
     const int p_min = pos0 + one(a.by_g.div(row0)), p_max = pos0 + one(a.by_g.div(min(row0 + RT, q.rows) - 1));
     const int see_lo = a.window ? max(0, p_min - a.window + 1) : 0, see_hi = p_max + 1;     // keys that some row of the tile sees
     const int all_lo = a.window ? p_max - a.window + 1 : 0;                                 // keys all_lo .. p_min are seen by all of them
@@ -219,7 +241,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     for (int mb = 0; mb < MB; ++mb) {
       const int r = min(row0 + 16 * mb + lo, q.rows - 1), tok = (int)a.by_g.div(r);
       pos[mb] = pos0 + tok;
-      const __bf16* src = a.Q + (q.q0 + tok) * a.q_t + ((int)h * a.g + r - tok * a.g) * a.q_h;
+      const __bf16* src = a.Q + (q.q0 + tok) * a.q_t + (h * a.g + r - tok * a.g) * a.q_h;
 #pragma unroll
       for (int st = 0; st < S::NS; ++st)
         qf[mb][st] = *(const bf16x8*)(src + (E4M3 ? 64 * (st >> 1) + 16 * quarter + 8 * (st & 1) : 32 * st + 8 * quarter));
@@ -230,18 +252,18 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       const int key = q.first + 16 * (64 * chunk + lane);
       return key < see_hi ? a.b.page(seq, key) : -1;
     };
-    int chunk = s0 >> 3, ids = page_ids(chunk), ids_next = page_ids(chunk + 1);
+    int chunk = s0 >> kChunkLog2, ids = page_ids(chunk), ids_next = page_ids(chunk + 1);
     auto issue = [&](int s, StepRegs<S::NK>& x, int buf) {
-      if ((s >> 3) != chunk) {
+      if ((s >> kChunkLog2) != chunk) {
         ++chunk;
         ids = ids_next;
         ids_next = page_ids(chunk + 1);
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int id = __builtin_amdgcn_readlane(ids, (8 * s + 2 * wave + j) & 63);
-        const int key0 = q.first + 16 * (8 * s + 2 * wave + j);
-        const long long row = a.b.row(max(id, 0), (int)h, key0);
+        const int id = __builtin_amdgcn_readlane(ids, (kBlocks * s + 2 * wave + j) & 63);
+        const int key0 = q.first + 16 * (kBlocks * s + 2 * wave + j);
+        const long long row = a.b.row(max(id, 0), h, key0);
         const char* kr = a.kp + (row + lo) * RB + 16 * quarter;
 #pragma unroll
         for (int i = 0; i < S::NK; ++i) x.k[j][i] = ONCE ? __builtin_nontemporal_load((const u32x4*)(kr + 64 * i)) : *(const u32x4*)(kr + 64 * i);
@@ -269,12 +291,12 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     }
 
     auto compute = [&](int s, int ids_s, const StepRegs<S::NK>& x, int buf) {
-      const int key0 = q.first + 16 * (8 * s + 2 * wave);
+      const int key0 = q.first + 16 * (kBlocks * s + 2 * wave);
       bool masked[2], dead[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int k0 = key0 + 16 * j;
-        const bool gone = __builtin_amdgcn_readlane(ids_s, (8 * s + 2 * wave + j) & 63) < 0;
+        const bool gone = __builtin_amdgcn_readlane(ids_s, (kBlocks * s + 2 * wave + j) & 63) < 0;
         dead[j] = gone || k0 >= see_hi || k0 + 15 < see_lo;
         masked[j] = dead[j] || k0 + 15 > p_min || k0 < all_lo;
       }
@@ -372,7 +394,13 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       if (s + 2 >= s1) break;
     }
 
-    // ---- the four wavefronts meet
+    // ---- the wavefronts meet
+    const auto max_of = [&](int r) {
+      float mt = ml[0][r][0];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) mt = fmaxf(mt, ml[w][r][0]);
+      return mt;
+    };
     __syncthreads();                                     // (the rings are free)
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -388,32 +416,32 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
       const int r = 16 * mb + lo;
-      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0])), alpha = fast_exp2(m[mb] - mt);
+      const float mt = max_of(r), alpha = fast_exp2(m[mb] - mt);
 #pragma unroll
       for (int dt = 0; dt < S::ND; ++dt) *(f32x4*)(meet + (wave * RT + r) * S::OS + 16 * dt + 4 * quarter) = o[mb][dt] * alpha;
     }
     __syncthreads();
-    const bool complete = s0 == 0 && s1 == q.steps;
+    const bool complete = WHOLE || (s0 == 0 && s1 == q.steps);
     const int side = s0 == 0 ? 1 : 0;
     if (!complete && tid == side) {
       const uint32_t begin = u - s0, first = begin / share;
-      a.cut[2 * block + side] = Cut{(int)((begin + q.steps - 1) / share - first) + 1, (int)(block - first), q.q0, (int)h, row0, min(RT, q.rows - row0)};
+      a.cut[2 * block + side] = Cut{(int)((begin + q.steps - 1) / share - first) + 1, (int)(block - first), q.q0, h, row0, min(RT, q.rows - row0)};
     }
     const long long slot = 2LL * block + side;
-    for (int task = tid; task < RT * (D / 8); task += 256) {
+    for (int task = tid; task < RT * (D / 8); task += 64 * NW) {
       const int r = task / (D / 8), col = 8 * (task % (D / 8));
       if (row0 + r >= q.rows) continue;
-      const float mt = fmaxf(fmaxf(ml[0][r][0], ml[1][r][0]), fmaxf(ml[2][r][0], ml[3][r][0]));
+      const float mt = max_of(r);
       float lt = 0.f;
       f32x4 v[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < NW; ++w) {
         lt += ml[w][r][1] * fast_exp2(ml[w][r][0] - mt);
         v[0] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col);
         v[1] += *(const f32x4*)(meet + (w * RT + r) * S::OS + col + 4);
       }
       if (complete) {
-        const int tok = (int)a.by_g.div(row0 + r), head = (int)h * a.g + row0 + r - tok * a.g;
+        const int tok = (int)a.by_g.div(row0 + r), head = h * a.g + row0 + r - tok * a.g;
         const float inv = lt > 0.f ? 1.0f / lt : 0.f;
         bf16x8 out;
 #pragma unroll
@@ -431,11 +459,15 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       }
     }
     __syncthreads();
-    u += units;
-    in_seq += units;
-    if (in_seq >= (uint32_t)(Hkv * q.tiles) * span) {
-      ++seq;
-      in_seq = 0;
+    if constexpr (WHOLE) {
+      whole_tile += a.whole;
+    } else {
+      u += units;
+      in_seq += units;
+      if (in_seq >= (uint32_t)(Hkv * q.tiles) * span) {
+        ++seq;
+        in_seq = 0;
+      }
     }
   }
 }

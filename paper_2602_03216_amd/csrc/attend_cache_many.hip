@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
   __shared__ __attribute__((aligned(1024))) char smem[kRings > kFewLds ? kRings : kFewLds];
   if constexpr (FEW) {
     if (blockIdx.x >= grid) {
-      few_rows<D, E4M3, 1, true>(a, smem, blockIdx.x - grid);
+      few_rows<D, E4M3, 1, true, false>(a, smem, blockIdx.x - grid);
       return;
     }
   }
