@@ -564,8 +564,9 @@ int tsa_rotary(const tsa_rotary_desc* d, const void* Q, const void* K, const int
   for (int i = 0; i < d->rot / 2; ++i) {
     if (!std::isfinite(d->freq[i])) return fail(TSA_ERR_ARG, "freq[%d] is not finite", i);
     // whole turns per position change nothing; what is left, in [0, 1), as a fraction of 2^64
-    const long double turns = (long double)d->freq[i] / 6.283185307179586476925286766559L, part = turns - std::floor(turns);
-    a.turns[i] = part >= 1.0L ? 0 : (uint64_t)std::ldexp(part, 64);
+    const long double turns = (long double)d->freq[i] / 6.283185307179586476925286766559L;
+    const long double part = turns >= 0.0L && turns < 1.0L ? turns : turns - std::floor(turns);
+    a.turns[i] = part >= 1.0L ? 0 : (uint64_t)(part * 0x1p64L);
   }
   return hip_status(tsa::launch_rotary(a, (hipStream_t)stream), "tsa_rotary");
 }
