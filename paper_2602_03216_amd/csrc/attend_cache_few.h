@@ -75,7 +75,7 @@ struct Shape {
   static constexpr int kTiles = NW * kRing > kMerge ? NW * kRing : kMerge;
   struct Tail {
     float ml[NW][RT][2];                                  // where the wavefronts meet: max and sum of every row
-    uint32_t scan[4], place[2];
+    uint32_t scan[16], place[2];
   };
   static constexpr int kLds = kTiles + (int)sizeof(Tail);
   // 16-byte piece p of row r of V is kept at p ^ swizzle(r): the 32 lanes that a transposing read serves at once then touch all banks
@@ -84,6 +84,34 @@ struct Shape {
     return RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1;
   }
 };
+
+// Sums of x over lanes 0 .. this one, in six additions without LDS.
+__device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
+  const auto add = [&](uint32_t y) { x += y; };
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));       // from 1, 2, 4, 8 lanes below, inside 16
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));       // lane 15 of a row into the next one, lane 31 into the upper half
+  add(__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+  return x;
+}
+// Sums over the wavefront, or over all four of the workgroup.
+template <int N>
+__device__ __forceinline__ void sum_up(uint32_t (&x)[N], bool alone, uint32_t* scan, int lane, int wave) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_readlane(sum_up_to_lane(x[i]), 63);
+  if (alone) return;
+  __syncthreads();
+  if (lane < N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (lane == i) scan[4 * i + wave] = x[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = one(scan[4 * i] + scan[4 * i + 1] + scan[4 * i + 2] + scan[4 * i + 3]);
+}
 
 // K of a step in registers, and the exponents of both.
 template <int NK>
@@ -124,26 +152,32 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
     const auto over_mine = [&](auto&& f) {
       for (int i = i0; i < i1; ++i) f(i, per == 1 ? own : sequence(a, i, RT));
     };
-    const auto sum_up = [&](uint32_t x) -> uint32_t {
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-      if (!alone) {
-        __syncthreads();
-        if (lane == 0) scan[wave] = x;
-        __syncthreads();
-        x = scan[0] + scan[1] + scan[2] + scan[3];
-      }
-      return one(x);
-    };
-    uint32_t mine = 0;
+    uint32_t mine = 0, sum[1];
     over_mine([&](int, const Seq& q) { mine += q.units(Hkv, 1); });
-    uint32_t total = sum_up(mine);
-    share = (total + kShares - 1) / kShares;
+    sum[0] = mine;
+    sum_up(sum, alone, scan, lane, wave);
+    share = (sum[0] + kShares - 1) / kShares;
     if (share > 1) {
-      for (int k = 0; k < 4 && of == 1; ++k) {
-        uint32_t parts = 0;                                // shares that whole ones of share + k steps make
-        over_mine([&](int, const Seq& q) { parts += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k - 1) / (share + k)); });
-        if (sum_up(parts) <= (uint32_t)kShares) of = (int)share + k;
+      // shares that whole ones of share + k steps make; over the workgroup a sum is two barriers, so all k at once (2000 x 100 keys 109 -> 98 us)
+      const auto count = [&](auto& parts, int k0) {
+        over_mine([&](int, const Seq& q) {
+#pragma unroll
+          for (int k = 0; k < (int)(sizeof(parts) / 4); ++k) parts[k] += (uint32_t)(Hkv * q.tiles) * ((q.steps + share + k0 + k - 1) / (share + k0 + k));
+        });
+        sum_up(parts, alone, scan, lane, wave);
+      };
+      if (alone) {
+        for (int k = 0; k < 4 && of == 1; ++k) {
+          uint32_t parts[1] = {0};
+          count(parts, k);
+          if (parts[0] <= (uint32_t)kShares) of = (int)share + k;
+        }
+      } else {
+        uint32_t parts[4] = {0, 0, 0, 0};
+        count(parts, 0);
+#pragma unroll
+        for (int k = 3; k >= 0; --k)
+          if (parts[k] <= (uint32_t)kShares) of = (int)share + k;
       }
       if (of > 1) {
         share = of;
@@ -152,12 +186,7 @@ __device__ __forceinline__ void few_rows(const Args& a, char* smem, unsigned blo
       }
     }
     if (tid < 2) a.cut[2 * block + tid].parts = 0;
-    uint32_t upto = mine;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const uint32_t o = __shfl_up(upto, m);
-      if (lane >= m) upto += o;
-    }
+    uint32_t upto = sum_up_to_lane(mine), total;
     of = one(of);
     share = one(share);
     u = block * share;
