@@ -9,7 +9,7 @@
 // equal shares, one per workgroup; lengths are known on the device only, so every workgroup sums them up itself and finds its
 // place.  A share that covers only a part of a row tile's keys leaves its running max, sum and output in the workspace, and a second launch
 // joins them; whole ones are written at once.  Where contexts are short and few, a workgroup takes a whole tile instead (WHOLE).
-//   A wavefront takes 32 keys of a step, with a softmax of its own; the four meet at the end of a segment.  S^T = K Q^T on
+//   A wavefront takes 32 keys of a step, with a softmax of its own; they meet at the end of a segment.  S^T = K Q^T on
 // v_mfma_f32_16x16x32_bf16: rows = keys, columns = the tile's rows, so a lane keeps one row's max and sum.  K goes from memory straight
 // into the registers of that product (a lane's 16 bytes are its operand).  O^T = V^T P^T takes the probabilities as the lane holds them: its
 // contraction index runs over keys 4 q .. 4 q + 3 of the first 16 and of the second 16 keys (q = lane / 16), and V^T comes out of LDS
