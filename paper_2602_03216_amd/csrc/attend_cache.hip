@@ -166,7 +166,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kFewRows = 64;
 
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
-// and for many the slots for row tiles and the parts that their keys are cut into so that 512 workgroups run.
+// and for many the slots for row tiles and the parts that their keys are cut into so that up to 512 workgroups run.
 struct Plan {
   bool few, many, fits, once, whole;
   int mb, tiles, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
@@ -203,9 +203,14 @@ Plan plan_of(const CacheArgs& c) {
   p.whole = !p.many && p.mb == 1 && whole_tiles <= 256 && seen <= (512 << ((c.d == 64 || c.e4m3) + (whole_tiles >= 128)));
   p.shares = p.whole ? 1 : 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
-  const long long tiles = (((long long)c.n_tokens * g + kManyRows - 1) / kManyRows) * c.Hkv;
+  // Row tiles, as if sequences of the most tokens made up the rows; parts as many as run at once with them (two workgroups a CU).  One part more, so that no
+  // place stays empty, starts a second round: 32 / 8 heads, bf16, us with the last part that fits / one more: 300 tokens over 6000 keys 51 / 61, 700 over
+  // 16384 213 / 269, 4 x 300 over 6000 150 / 168, with a window of 1024 40 / 60; twice the parts: 63, 211, 166, 61.
+  const auto tiles_of = [&](long long tokens) { return (tokens * g + kManyRows - 1) / kManyRows; };
+  const long long full = most > 0 ? c.n_tokens / most : 0;
+  const long long tiles = c.Hkv * (full > 0 && full <= c.n_seqs ? full * tiles_of(most) + tiles_of(c.n_tokens - full * most) : tiles_of(c.n_tokens));
   const long long most_parts = cap / (kTile * kPartTiles);
-  long long s = (512 + tiles - 1) / (tiles > 0 ? tiles : 1);
+  long long s = 512 / (tiles > 0 ? tiles : 1);
   if (s > most_parts) s = most_parts;
   p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
   return p;
