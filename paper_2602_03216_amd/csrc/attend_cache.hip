@@ -211,6 +211,10 @@ Plan plan_of(const CacheArgs& c) {
   const long long tiles = c.Hkv * (full > 0 && full <= c.n_seqs ? full * tiles_of(most) + tiles_of(c.n_tokens - full * most) : tiles_of(c.n_tokens));
   const long long most_parts = cap / (kTile * kPartTiles);
   long long s = 512 / (tiles > 0 ? tiles : 1);
+  // Where those leave a quarter of the places empty: parts that fill two rounds, as long as they are long (28 / 4 heads, 1500 tokens, one part / three:
+  // over 16384 keys bf16 369 / 338, d = 64 in 8 bits 280 / 219; over 6000 137 / 136, 103 / 90; over 2500 58 / 71, 47 / 51).
+  const long long two = tiles > 0 ? 1024 / tiles : 0;
+  if (tiles * s < 384 && tiles * two >= 896 && seen >= 1536 * two) s = two;
   if (s > most_parts) s = most_parts;
   p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
   return p;
