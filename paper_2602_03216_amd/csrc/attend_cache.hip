@@ -166,7 +166,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kFewRows = 64;
 
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
-// and for many the slots for row tiles and the parts that their keys are cut into so that up to 512 workgroups run.
+// and for many the slots for row tiles and the parts that their keys are cut into.
 struct Plan {
   bool few, many, fits, once, whole;
   int mb, tiles, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
@@ -203,18 +203,22 @@ Plan plan_of(const CacheArgs& c) {
   p.whole = !p.many && p.mb == 1 && whole_tiles <= 256 && seen <= (512 << ((c.d == 64 || c.e4m3) + (whole_tiles >= 128)));
   p.shares = p.whole ? 1 : 256 * per_cu(c.d, c.e4m3, p.mb);
   p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
-  // Row tiles, as if sequences of the most tokens made up the rows; parts as many as run at once with them (two workgroups a CU).  One part more, so that no
+  // Row tiles, as if sequences of the most tokens made up the rows; parts as many as run at once with them (two workgroups a CU, of d = 64 in bf16 three).  One part more, so that no
   // place stays empty, starts a second round: 32 / 8 heads, bf16, us with the last part that fits / one more: 300 tokens over 6000 keys 51 / 61, 700 over
   // 16384 213 / 269, 4 x 300 over 6000 150 / 168, with a window of 1024 40 / 60; twice the parts: 63, 211, 166, 61.
   const auto tiles_of = [&](long long tokens) { return (tokens * g + kManyRows - 1) / kManyRows; };
   const long long full = most > 0 ? c.n_tokens / most : 0;
   const long long tiles = c.Hkv * (full > 0 && full <= c.n_seqs ? full * tiles_of(most) + tiles_of(c.n_tokens - full * most) : tiles_of(c.n_tokens));
   const long long most_parts = cap / (kTile * kPartTiles);
-  long long s = 512 / (tiles > 0 ? tiles : 1);
+  const long long places = c.d == 64 && !c.e4m3 ? 768 : 512;
+  long long s = places / (tiles > 0 ? tiles : 1);
   // Where those leave a quarter of the places empty: parts that fill two rounds, as long as they are long (28 / 4 heads, 1500 tokens, one part / three:
   // over 16384 keys bf16 369 / 338, d = 64 in 8 bits 280 / 219; over 6000 137 / 136, 103 / 90; over 2500 58 / 71, 47 / 51).
-  const long long two = tiles > 0 ? 1024 / tiles : 0;
-  if (tiles * s < 384 && tiles * two >= 896 && seen >= 1536 * two) s = two;
+  const long long two = tiles > 0 ? 2 * places / tiles : 0;
+  if (4 * tiles * s < 3 * places && 4 * tiles * two >= 7 * places && seen >= 1536 * two) s = two;
+  // ... and three parts where the tiles are a few more than the places (32 / 8 heads, 2176 tokens, bf16, one part / three: over 16384 keys 693 / 576, over 6000
+  // 215 / 218).
+  if (tiles > places && 3 * tiles <= 4 * places && seen >= 8192) s = 3;
   if (s > most_parts) s = most_parts;
   p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
   return p;
