@@ -346,7 +346,9 @@ enum { TSA_CACHE_BF16 = 0, TSA_CACHE_E4M3 = 1 };
 typedef struct tsa_cache_desc {
   int32_t n_seqs;           /* >= 1 */
   int32_t n_tokens;         /* rows of the packed tensors, >= 0 (0: nothing to do) */
-  int32_t max_q;            /* most new tokens of a sequence, as far as the caller knows (0: no idea); the result does not depend on it */
+  int32_t max_q;            /* most new tokens of a sequence, as far as the caller knows (0: no idea).  Any value is right; what is launched and the
+                             * attention's workspace go by it: without it, or above 64 rows (tokens times Hq / Hkv), a call is prepared for prompts
+                             * (64 single tokens over 16384 keys, 32 / 8 heads, d = 128: 60 MB instead of 9; never above 300 MB) */
   int32_t Hq, Hkv;          /* Hq % Hkv == 0 */
   int32_t d;                /* 64 or 128 */
   int32_t page_size;        /* 16, 32, 64, 128 or 256 */

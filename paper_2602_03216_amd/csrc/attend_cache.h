@@ -20,6 +20,8 @@ constexpr float kLag = attend_detail::kLazy;             // log2 units that the 
 constexpr int kStep = 128;                               // keys of a step
 constexpr int kTile = 64;                                // many rows: keys of a tile
 constexpr int kPartTiles = 8;                            // ... and fewest tiles of a part
+constexpr int kManyRows = 128;                           // ... and rows of a workgroup
+constexpr int kFewRows = 64;                             // sequences of at most so many rows (new tokens times heads of a group) are dealt by keys, the others by rows
 
 // A row tile of which a share has a part only: its parts (0: there is none), which one the share has, and the tile's rows.
 struct Cut {
@@ -45,7 +47,7 @@ struct Args {
   float* part_ml;                // [2 shares][rt][2]
   int rt, shares, whole;         // rows of a tile; whole tiles of a sequence that run side by side
   // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
-  int few, splits, slots;
+  int few, splits, slots, by_rows;                       // (by_rows: which slots a sequence has, see first_slot)
   float* many_o;                 // [slots][Hkv][splits][128][d]
   float* many_ml;                // [slots][Hkv][splits][128][2]
   int split_log2, vheads_per_xcd;
@@ -85,7 +87,6 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) 
 __device__ const u32x4 g_zeros[16] = {};                 // a row of V for keys that nobody sees
 
 // Many rows: what the workgroups of one row tile (128 rows of one sequence and KV head) have in common.
-constexpr int kManyRows = 128;
 struct ManyTile {
   int q0, q_len, kv, rows, row0;
   int p_min, p_max;              // positions of its first and last row
@@ -114,9 +115,16 @@ __device__ __forceinline__ ManyTile many_tile(const Args& a, int seq, int tile) 
   x.parts = one(x.per ? (x.tiles + x.per - 1) / x.per : 1);
   return x;
 }
-// First slot of a sequence's row tiles in the grid: rows in front of it, in tiles, and one more for every sequence, which is never less than
-// what the sequences in front of it take.
-__device__ __forceinline__ int first_slot(const Args& a, int seq) { return a.b.first(seq) * a.g / kManyRows + seq; }
+// First slot of a sequence's row tiles in the grid and in the workspace, from the rows x in front of it alone (a sum over the batch would be in front of
+// every workgroup's first load).  Either x in tiles and one more for every sequence: right for all, and most of it empty where many sequences
+// have few rows.  Or x / 64.5: a sequence of r > 64 rows has ceil(r / 128) tiles, never more than floor(2 r / 129), so it reaches no slot of the next one;
+// sequences with fewer rows have none.  The host takes what needs fewer slots: 64 single tokens of a caller who does not know that they are single have
+// 3 slots a head instead of 66, and their parts 60 MB instead of 1.1 GB.
+static_assert(kManyRows == 2 * kFewRows, "2 r / (kManyRows + 1) holds the tiles of r > kFewRows rows");
+__device__ __forceinline__ int first_slot(const Args& a, int seq) {
+  const int rows = a.b.first(seq) * a.g;                 // (at most 2^30)
+  return a.by_rows ? (int)(2u * (unsigned)rows / (kManyRows + 1)) : rows / kManyRows + seq;
+}
 
 }  // namespace attend_cache_detail
 

@@ -162,13 +162,10 @@ __global__ __launch_bounds__(256) void join_many_rows(Args a) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Sequences with at most this many rows (new tokens times heads of a group) are dealt by keys, the others by rows.
-constexpr int kFewRows = 64;
-
 // How a call is cut, from what the host knows: whether any sequence may have many rows, rows of a tile and shares of the ones that have few,
 // and for many the slots for row tiles and the parts that their keys are cut into.
 struct Plan {
-  bool few, many, fits, once, whole;
+  bool few, many, fits, once, whole, by_rows;
   int mb, tiles, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
 };
 Plan plan_of(const CacheArgs& c) {
@@ -202,7 +199,10 @@ Plan plan_of(const CacheArgs& c) {
   const long long whole_tiles = (long long)c.n_seqs * c.Hkv * p.tiles;
   p.whole = !p.many && p.mb == 1 && whole_tiles <= 256 && seen <= (512 << ((c.d == 64 || c.e4m3) + (whole_tiles >= 128)));
   p.shares = p.whole ? 1 : 256 * per_cu(c.d, c.e4m3, p.mb);
-  p.slots = (int)((long long)c.n_tokens * g / kManyRows) + c.n_seqs;
+  // slots for row tiles, the fewer of two kinds (first_slot)
+  const long long by_seq = rows_all / kManyRows + c.n_seqs, by_rows = 2 * rows_all / (kManyRows + 1);
+  p.by_rows = p.few && by_rows < by_seq;
+  p.slots = (int)(p.by_rows ? by_rows : by_seq);
   // Row tiles, as if sequences of the most tokens made up the rows; parts as many as run at once with them (two workgroups a CU, of d = 64 in bf16 three).  One part more, so that no
   // place stays empty, starts a second round: 32 / 8 heads, bf16, us with the last part that fits / one more: 300 tokens over 6000 keys 51 / 61, 700 over
   // 16384 213 / 269, 4 x 300 over 6000 150 / 168, with a window of 1024 40 / 60; twice the parts: 63, 211, 166, 61.
@@ -298,7 +298,7 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.rt = 16 * p.mb; a.shares = p.shares; a.whole = p.tiles; a.slots = p.slots; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.shares = p.shares; a.whole = p.tiles; a.slots = p.slots; a.by_rows = p.by_rows; a.splits = p.splits;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }
