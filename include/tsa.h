@@ -381,7 +381,8 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
  *   Q [n_tokens,Hq,d] bf16;  O [n_tokens,Hq,d] bf16 out;  lse [n_tokens,Hq] fp32 out or NULL (natural-log sum-exp of the scaled logits)
  *   A token that sees no key gets zeros and -infinity.  O overlaps no input.  A NaN or an infinity in a row of V may reach tokens of the call
  *   that do not see it; in K it reaches those that do.
- *   ws: tsa_attend_cache_workspace_bytes(desc) bytes; its contents need not be kept between calls
+ *   ws: tsa_attend_cache_workspace_bytes(desc) bytes (0: refused, as tsa_last_error() says); its contents need not be kept between calls
+ *   Not supported: Hkv * (n_seqs + (rows with at most 64 a sequence) / 16) * (max_pages * page_size / 128 + 2048) from 4e9 on
  * Arithmetic as in tsa_attend; 8-bit rows are widened exactly. The same inputs give the same bits. */
 size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc);
 int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,

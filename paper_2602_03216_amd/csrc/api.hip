@@ -702,10 +702,20 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
   return hip_status(tsa::launch_cache_read(c, L, K, V, (hipStream_t)stream), "tsa_cache_read");
 }
 
+namespace {
+
+int attend_cache_need(const tsa::CacheArgs& c, size_t* need) {
+  *need = tsa::attend_cache_ws_bytes(c);
+  if (*need == 0) return fail(TSA_ERR_UNSUPPORTED, "n_seqs * Hkv * max_pages * page_size is too large: keys are counted in 2^32 steps of 128");
+  return TSA_OK;
+}
+
+}  // namespace
+
 size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc) {
   tsa::CacheArgs c;
-  if (check_cache_desc(desc, &c) != TSA_OK) return 0;
-  return tsa::attend_cache_ws_bytes(c);
+  size_t need;
+  return check_cache_desc(desc, &c) || attend_cache_need(c, &need) ? 0 : need;
 }
 
 int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
@@ -718,8 +728,8 @@ int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pa
   if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(O, "O")) || (rc = check_ints(cu_q, "cu_q"))) return rc;
   if (lse && ((uintptr_t)lse & 3u)) return fail(TSA_ERR_ARG, "lse is not 4-byte aligned");
   if ((rc = check_cache(&c, k_pages, v_pages, k_scales, v_scales, kv_len, page_table))) return rc;
-  const size_t need = tsa::attend_cache_ws_bytes(c);
-  if (need == 0) return fail(TSA_ERR_UNSUPPORTED, "n_seqs * Hkv * max_pages * page_size is too large: keys are counted in 2^32 steps of 128");
+  size_t need;
+  if ((rc = attend_cache_need(c, &need))) return rc;
   if ((rc = check_ws(ws, ws_bytes, need))) return rc;
   if (O == Q) return fail(TSA_ERR_ARG, "O is Q");
   c.cu_q = cu_q;

@@ -31,3 +31,14 @@ def test_tokens_of_a_caller_who_does_not_know_that_they_are_single():
     assert _bytes(64, 64, 0, 16384) < 100e6
     assert _bytes(4096, 32, 0, 131072) < 100e6
     assert _bytes(256, 272, 17, 16384) < 100e6
+
+
+def test_a_size_that_is_refused_says_why():
+    """Its own reason, not the one of the call before it."""
+    lib = tsa.load_library()
+    assert _bytes(1, 1, 1, 1000, d=80) == 0 and "head dimension 80" in tsa.tsa_last_error()
+    big = tsa.make_cache_desc(1 << 19, 7, 32, 8, 128, 16, 10, 1 << 20)
+    assert lib.tsa_attend_cache_workspace_bytes(ctypes.byref(big)) == 0 and "max_pages" in tsa.tsa_last_error()
+    assert _bytes(1, 1, 1, 1000, d=80) == 0
+    with pytest.raises(tsa.TsaError, match="max_pages"):
+        tsa.alloc_attend_cache_workspace(big)
