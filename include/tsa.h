@@ -353,7 +353,9 @@ typedef struct tsa_cache_desc {
   int32_t d;                /* 64 or 128 */
   int32_t page_size;        /* 16, 32, 64, 128 or 256 */
   int32_t n_pages;          /* of the pool, >= 1 */
-  int32_t max_pages;        /* of a sequence, >= 1; max_pages * page_size < 2^30 */
+  int32_t max_pages;        /* of a sequence, >= 1; max_pages * page_size < 2^30.  How single and drafted tokens are dealt goes by it as the longest
+                             * context there may be: a table no wider than that is faster over short contexts (one token over 500 keys, 32 / 8
+                             * heads, bf16, 8.9 us with a table of 512 positions, 10.7 with one of 131072) */
   int32_t format;           /* TSA_CACHE_* */
   int32_t window;           /* attention: a query at position p sees the keys p - window < t <= p; 0: all t <= p */
   float scale;              /* attention: softmax scale; 0 means 1/sqrt(d) */

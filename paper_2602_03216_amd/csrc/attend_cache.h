@@ -46,12 +46,13 @@ struct Args {
   float* part_o;                 // [2 shares][rt][d]
   float* part_ml;                // [2 shares][rt][2]
   int rt, shares, whole;         // rows of a tile; whole tiles of a sequence that run side by side
-  // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts
-  int few, splits, slots, by_rows;                       // (by_rows: which slots a sequence has, see first_slot)
+  // sequences of more rows than `few` go the way of many rows: 128 of them per workgroup, a tile's keys in up to `splits` parts, or `short_splits`
+  // where the sequence's new tokens see fewer than `long_keys` keys
+  int few, splits, short_splits, long_keys, slots, by_rows;      // (by_rows: which slots a sequence has, see first_slot)
   float* many_o;                 // [slots][Hkv][splits][128][d]
   float* many_ml;                // [slots][Hkv][splits][128][2]
   int split_log2, vheads_per_xcd;
-  FastDiv by_vheads, by_splits;
+  FastDiv by_vheads, by_slots;
 };
 
 // The same in all lanes, and kept in a scalar: the compiler forms quotients, and what is loaded or shuffled, in vector registers, and leaves everything
@@ -110,7 +111,8 @@ __device__ __forceinline__ ManyTile many_tile(const Args& a, int seq, int tile) 
   x.see_hi = x.p_max + 1;
   x.start = x.see_lo & ~15;
   x.tiles = max(0, (x.see_hi - x.start + kTile - 1) / kTile);
-  const int parts = max(1, min(a.splits, x.tiles / kPartTiles));
+  const int seen = a.window ? min(x.kv, a.window + x.q_len) : x.kv;
+  const int parts = max(1, min(seen < a.long_keys ? a.short_splits : a.splits, x.tiles / kPartTiles));
   x.per = one((x.tiles + parts - 1) / parts);
   x.parts = one(x.per ? (x.tiles + x.per - 1) / x.per : 1);
   return x;

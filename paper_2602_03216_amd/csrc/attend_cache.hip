@@ -166,7 +166,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // and for many the slots for row tiles and the parts that their keys are cut into.
 struct Plan {
   bool few, many, fits, once, whole, by_rows;
-  int mb, tiles, rows, shares, slots, splits;                   // rows: of a tile, as many as there will be
+  int mb, tiles, rows, shares, slots, splits, short_splits, long_keys;      // rows: of a tile, as many as there will be
 };
 Plan plan_of(const CacheArgs& c) {
   const int g = c.Hq / c.Hkv, most = c.max_q > 0 && c.max_q < c.n_tokens ? c.max_q : c.n_tokens;
@@ -211,16 +211,25 @@ Plan plan_of(const CacheArgs& c) {
   const long long tiles = c.Hkv * (full > 0 && full <= c.n_seqs ? full * tiles_of(most) + tiles_of(c.n_tokens - full * most) : tiles_of(c.n_tokens));
   const long long most_parts = cap / (kTile * kPartTiles);
   const long long places = c.d == 64 && !c.e4m3 ? 768 : 512;
-  long long s = places / (tiles > 0 ? tiles : 1);
-  // Where those leave a quarter of the places empty: parts that fill two rounds, as long as they are long (28 / 4 heads, 1500 tokens, one part / three:
+  const auto parts = [&](long long s) { return s > most_parts ? most_parts : s; };
+  const auto bounded = [](long long s) { return (int)(s < 1 ? 1 : s > kMostParts ? kMostParts : s); };
+  const long long s = places / (tiles > 0 ? tiles : 1);
+  p.splits = p.short_splits = bounded(parts(s));
+  p.long_keys = 0;
+  // Over long contexts more than that; how long they are, the device knows (the table may be a model's longest: 2176 tokens over 2500 keys, 32 / 8 heads, bf16,
+  // with a table of 131072 positions 94 us in the parts of a long context, 66 in those of a short one).
+  const auto over = [&](long long keys, long long more) {
+    if (seen < keys) return;
+    p.long_keys = (int)keys;
+    p.splits = bounded(parts(more));
+  };
+  // Where one round leaves a quarter of the places empty: parts that fill two rounds, as long as they are long (28 / 4 heads, 1500 tokens, one part / three:
   // over 16384 keys bf16 369 / 338, d = 64 in 8 bits 280 / 219; over 6000 137 / 136, 103 / 90; over 2500 58 / 71, 47 / 51).
   const long long two = tiles > 0 ? 2 * places / tiles : 0;
-  if (4 * tiles * s < 3 * places && 4 * tiles * two >= 7 * places && seen >= 1536 * two) s = two;
+  if (4 * tiles * s < 3 * places && 4 * tiles * two >= 7 * places) over(1536 * two, two);
   // ... and three parts where the tiles are a few more than the places (32 / 8 heads, 2176 tokens, bf16, one part / three: over 16384 keys 693 / 576, over 6000
   // 215 / 218).
-  if (tiles > places && 3 * tiles <= 4 * places && seen >= 8192) s = 3;
-  if (s > most_parts) s = most_parts;
-  p.splits = s < 1 ? 1 : s > kMostParts ? kMostParts : (int)s;
+  if (tiles > places && 3 * tiles <= 4 * places) over(8192, 3);
   return p;
 }
 
@@ -298,7 +307,8 @@ hipError_t launch_attend_cache(const CacheArgs& c, const void* Q, void* O, float
   a.part_o = (float*)(base + w.part_o);
   a.many_ml = (float*)(base + w.many_ml);
   a.many_o = (float*)(base + w.many_o);
-  a.rt = 16 * p.mb; a.shares = p.shares; a.whole = p.tiles; a.slots = p.slots; a.by_rows = p.by_rows; a.splits = p.splits;
+  a.rt = 16 * p.mb; a.shares = p.shares; a.whole = p.tiles; a.slots = p.slots; a.by_rows = p.by_rows;
+  a.splits = p.splits; a.short_splits = p.short_splits; a.long_keys = p.long_keys;
   if (c.d == 128) return c.e4m3 ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
   return c.e4m3 ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
 }

@@ -63,13 +63,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_many_rows(Args a, unsigned 
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 31, hi = lane >> 5;
 
-  // ---- workgroup -> KV head, row tile, part.  id % 8 is the XCD: the row tiles of a head stay on one (or a few) of them, the last ones first.
+  // ---- workgroup -> KV head, row tile, part.  id % 8 is the XCD: the row tiles of a head stay on one (or a few) of them, the last ones first.  All tiles' first
+  // parts are in front of all second ones, so that parts that a short context does not have stand at the end: between the others they spoil the spread over
+  // the CUs (2176 tokens over 6000 keys, 32 / 8 heads, a table of 131072 positions: 235 us, 218 so; without such parts no difference).
   const unsigned xcd = blockIdx.x & 7u, at = blockIdx.x >> 3;
   const unsigned rank = one(a.by_vheads.div(at)), vhead = xcd * a.vheads_per_xcd + (at - rank * a.vheads_per_xcd);
   const int h = (int)(vhead >> a.split_log2);
-  const unsigned item = (rank << a.split_log2) + (vhead & ((1u << a.split_log2) - 1u)), from_last = one(a.by_splits.div(item));
-  const int part = (int)(item - from_last * a.splits), slot = a.slots - 1 - (int)from_last;
-  if (slot < 0) return;
+  const unsigned item = (rank << a.split_log2) + (vhead & ((1u << a.split_log2) - 1u));
+  const int part = one(a.by_slots.div(item)), slot = a.slots - 1 - (int)(item - (unsigned)part * a.slots);
+  if (part >= a.splits) return;
   const int seq = one(last_up_to(a.b.n_seqs, slot, lane, [&](int i) { return first_slot(a, i); }));
   if (seq < 0 || seq >= a.b.n_seqs) return;
   const ManyTile x = many_tile(a, seq, slot - one(first_slot(a, seq)));
@@ -460,7 +462,7 @@ hipError_t launch_attend_many(Args& a, int d, bool e4m3, int shares, hipStream_t
   const long long items = (long long)a.slots * a.splits, ranks = (items + (1 << log2) - 1) >> log2, grid = 8LL * a.vheads_per_xcd * ranks;
   if (grid + shares > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   a.by_vheads = FastDiv((uint32_t)a.vheads_per_xcd, (uint64_t)a.vheads_per_xcd * (ranks + 1));
-  a.by_splits = FastDiv((uint32_t)a.splits, (uint64_t)items + 8);
+  a.by_slots = FastDiv((uint32_t)a.slots, (uint64_t)items + 8);
   if (d == 128) {
     if (e4m3) launch_rows<128, true>(a, (unsigned)grid, shares, st);
     else launch_rows<128, false>(a, (unsigned)grid, shares, st);

@@ -79,3 +79,16 @@ def test_every_rule_for_the_parts(tsa, name, e4m3):  # noqa: F811
     O, lse = b.run(tsa)
     check_some(b, O, lse, [0, 13, 31])
     assert np.isfinite(lse.cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("new,kv,d,e4m3,window", [(1270, 2560, 128, 0, 0), (1270, 2560, 64, 1, 0), (2110, 2560, 128, 0, 0), (2110, 2560, 128, 1, 0), (1270, 3840, 128, 0, 1200),
+                                                  (1270, 5120, 128, 0, 0), (3150, 3200, 64, 0, 0)])
+def test_a_wide_table_over_short_contexts(tsa, new, kv, d, e4m3, window):  # noqa: F811
+    """A prompt's parts go by its length: a table of as many pages as a model can have and one that ends with the context give the same bits."""
+    b = Batch(8400 + new + d, [new], [kv], 32, 1, d, 64, e4m3=e4m3, window=window)
+    want = b.run(tsa)
+    check_some(b, *want, [5])
+    b.tab = np.pad(b.tab, ((0, 0), (0, 2048 - b.max_pages)), constant_values=-1)
+    b.max_pages = 2048
+    got = b.run(tsa)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
