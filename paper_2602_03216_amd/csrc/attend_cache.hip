@@ -261,8 +261,10 @@ hipError_t launch(Args& a, const Plan& p, hipStream_t st) {
     return hipGetLastError();
   }
   if (p.few && !both) {
-    if (p.mb == 4) attend_few_rows<D, E4M3, 4, true><<<p.shares, 256, 0, st>>>(a);
-    else if (p.mb == 2) {
+    if (p.mb == 4) {
+      if constexpr (!(E4M3 && D == 128)) attend_few_rows<D, E4M3, 4, true><<<p.shares, 256, 0, st>>>(a);
+      else return hipErrorInvalidConfiguration;            // (those have tiles of at most 32 rows)
+    } else if (p.mb == 2) {
       bool once = true;
       if constexpr (E4M3 && D == 128) once = p.once;     // (the only ones whose 33 to 64 rows are not one tile)
       if (once) attend_few_rows<D, E4M3, 2, true><<<p.shares, 256, 0, st>>>(a);
