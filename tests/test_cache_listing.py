@@ -37,3 +37,28 @@ def test_every_kernel_is_one_that_a_call_can_reach(kernels):
     assert {k[1] for k in kernels if k[0] == "attend_whole_tiles"} == set(both)
     assert {k[1] for k in kernels if k[0] == "attend_many_rows"} == {(*x, f) for x in both for f in ("false", "true")}
     assert {k[1] for k in kernels if k[0] in ("join_few_rows", "join_many_rows")} == {("64",), ("128",)}
+
+
+def _loads_to_lds(code):
+    return [i for i, line in enumerate(code) if line.startswith("global_load_lds")]
+
+
+def test_every_load_to_lds_has_its_wait_states(kernels, monkeypatch):
+    """Five between a vector instruction that wrote m0 or the scalar base of a load and the load, which is inline assembly that the compiler's own hazard
+    pass does not look into (its vector address needs none)."""
+    monkeypatch.setattr(listing, "_loads", _loads_to_lds)
+    for (name, args), code in kernels.items():
+        if not name.startswith("attend"):
+            continue
+        few = name != "attend_many_rows" or args[2] == "true"
+        # (8 bits with many rows pass the registers)
+        assert len(_loads_to_lds(code)) >= (4 if few or args[1] == "false" else 0), (name, args)
+        assert not listing._short_waits(code), (name, args, listing._short_waits(code)[:3])
+
+
+def test_the_search_sees_these_loads(monkeypatch):
+    """on listings made up here"""
+    monkeypatch.setattr(listing, "_loads", _loads_to_lds)
+    plain, based = "global_load_lds_dwordx4 v[2:3], off nt", "global_load_lds_dwordx4 v2, s[4:5]"
+    assert listing._short_waits(["v_readfirstlane_b32 m0, v2", "s_nop 3", plain]) and listing._short_waits(["v_readlane_b32 s5, v2, 1", "s_nop 0", based])
+    assert not listing._short_waits(["v_readfirstlane_b32 m0, v2", "s_nop 4", plain]) and not listing._short_waits(["v_readlane_b32 s5, v2, 1", plain])
