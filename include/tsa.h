@@ -358,7 +358,7 @@ typedef struct tsa_cache_desc {
                              * heads, bf16, 8.9 us with a table of 512 positions, 10.7 with one of 131072) */
   int32_t format;           /* TSA_CACHE_* */
   int32_t window;           /* attention: a query at position p sees the keys p - window < t <= p; 0: all t <= p */
-  float scale;              /* attention: softmax scale; 0 means 1/sqrt(d) */
+  float scale;              /* attention: softmax scale, 2^-100 to 2^30; 0 means 1/sqrt(d) */
   /* Element strides of a token and of a head in the packed tensors: both 0 means contiguous; multiples of 8, row (token) strides not 0 */
   int64_t q_stride_t, q_stride_h;
   int64_t k_stride_t, k_stride_h;
@@ -385,7 +385,8 @@ int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* 
  *   that do not see it; in K it reaches those that do.
  *   ws: tsa_attend_cache_workspace_bytes(desc) bytes (0: refused, as tsa_last_error() says); its contents need not be kept between calls
  *   Not supported: Hkv * (n_seqs + (rows with at most 64 a sequence) / 16) * (max_pages * page_size / 128 + 2048) from 4e9 on
- * Arithmetic as in tsa_attend; 8-bit rows are widened exactly. The same inputs give the same bits. */
+ * Arithmetic as in tsa_attend: logits of up to 2^30 in magnitude, values of V that are 0 or between 2^-100 and 2^100 (8 bits: the row's power of two goes
+ * into the probability, which is rounded to bf16).  8-bit rows are widened exactly.  The same inputs give the same bits. */
 size_t tsa_attend_cache_workspace_bytes(const tsa_cache_desc* desc);
 int tsa_attend_cache(const tsa_cache_desc* desc, const void* Q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
                      const uint8_t* v_scales, const int32_t* cu_q, const int32_t* kv_len, const int32_t* page_table,

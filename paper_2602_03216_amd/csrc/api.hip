@@ -643,6 +643,8 @@ int check_cache_desc(const tsa_cache_desc* d, tsa::CacheArgs* c) {
   if (d->format != TSA_CACHE_BF16 && d->format != TSA_CACHE_E4M3) return fail(TSA_ERR_ARG, "format %d is none of TSA_CACHE_*", d->format);
   if (d->window < 0) return fail(TSA_ERR_ARG, "window must be >= 0");
   if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return fail(TSA_ERR_ARG, "scale must be finite and >= 0");
+  // the kernels divide by the scale, and take it times a product for what 32 bits hold to a fraction of a power of two
+  if (d->scale > 0.0f && (d->scale < 0x1p-100f || d->scale > 0x1p30f)) return fail(TSA_ERR_UNSUPPORTED, "scale %g: 0, or between 2^-100 and 2^30", (double)d->scale);
   c->n_seqs = d->n_seqs; c->n_tokens = d->n_tokens; c->max_q = d->max_q; c->Hq = d->Hq; c->Hkv = d->Hkv; c->d = d->d;
   c->page_log2 = __builtin_ctz((unsigned)d->page_size);
   c->n_pages = d->n_pages; c->max_pages = d->max_pages; c->e4m3 = d->format == TSA_CACHE_E4M3; c->window = d->window < (1 << 30) ? d->window : 0;      // (as long as any sequence: none)
