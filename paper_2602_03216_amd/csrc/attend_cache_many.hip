@@ -460,7 +460,7 @@ hipError_t launch_attend_many(Args& a, int d, bool e4m3, int shares, hipStream_t
   a.split_log2 = log2;
   a.vheads_per_xcd = a.b.Hkv / gcd;
   const long long items = (long long)a.slots * a.splits, ranks = (items + (1 << log2) - 1) >> log2, grid = 8LL * a.vheads_per_xcd * ranks;
-  if (grid + shares > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if ((grid + shares) * 64 * NW > 0xffffffffLL) return hipErrorInvalidConfiguration;      // (Q and O would be 137 GB each)
   a.by_vheads = FastDiv((uint32_t)a.vheads_per_xcd, (uint64_t)a.vheads_per_xcd * (ranks + 1));
   a.by_slots = FastDiv((uint32_t)a.slots, (uint64_t)items + 8);
   if (d == 128) {

@@ -112,9 +112,9 @@ struct ReadArgs {
 // rows without a page, are zeros.  One row per lane: a look-up, a load and a store that depend on one another, hidden by many wavefronts
 // (65536 tokens, 8 KV heads, d = 128, 8 bits: 75 us; two rows per lane 78, four 81, eight 98).
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a, int row_blocks, FastDiv by_blocks, FastDiv by_heads) {
+__global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a, int row_blocks, FastDiv by_blocks, FastDiv by_heads, unsigned first) {
   constexpr int LPR = D / 8, ROWS = 256 / LPR;             // lanes of a row, rows of a workgroup
-  const uint32_t sh = by_blocks.div(blockIdx.x), block = blockIdx.x - sh * (uint32_t)row_blocks;
+  const uint32_t at = blockIdx.x + first, sh = by_blocks.div(at), block = at - sh * (uint32_t)row_blocks;
   const uint32_t seq = by_heads.div(sh), h = sh - seq * (uint32_t)a.b.Hkv;
   const int p = (int)block * ROWS + (int)threadIdx.x / LPR, piece = threadIdx.x % LPR;
   if (p >= a.L) return;
@@ -183,16 +183,17 @@ hipError_t launch_cache_read(const CacheArgs& c, int L, void* K, void* V, hipStr
   a.kp = (const char*)c.kp; a.vp = (const char*)c.vp; a.ks = (const uint8_t*)c.ks; a.vs = (const uint8_t*)c.vs;
   a.K = (__bf16*)K; a.V = (__bf16*)V; a.L = L;
   const int rows = 2048 / c.d, blocks = (L + rows - 1) / rows;
-  const unsigned grid = (unsigned)c.n_seqs * c.Hkv * blocks;          // (checked to fit by the caller)
-  const FastDiv by_blocks(blocks, grid), by_heads(c.Hkv, (uint64_t)c.n_seqs * c.Hkv);
-  if (c.d == 128) {
-    if (c.e4m3) cache_read_kernel<128, true><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads);
-    else cache_read_kernel<128, false><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads);
-  } else {
-    if (c.e4m3) cache_read_kernel<64, true><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads);
-    else cache_read_kernel<64, false><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads);
-  }
-  return hipGetLastError();
+  const long long all = (long long)c.n_seqs * c.Hkv * blocks;          // (checked to fit 31 bits by the caller)
+  const FastDiv by_blocks(blocks, (uint64_t)all), by_heads(c.Hkv, (uint64_t)c.n_seqs * c.Hkv);
+  return launch_in_pieces(all, [&](unsigned first, unsigned grid) {
+    if (c.d == 128) {
+      if (c.e4m3) cache_read_kernel<128, true><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads, first);
+      else cache_read_kernel<128, false><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads, first);
+    } else {
+      if (c.e4m3) cache_read_kernel<64, true><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads, first);
+      else cache_read_kernel<64, false><<<grid, 256, 0, st>>>(a, blocks, by_blocks, by_heads, first);
+    }
+  });
 }
 
 }  // namespace tsa

@@ -42,11 +42,11 @@ __device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
 
 // UN units per row (d / 16), 1 << tt_log2 tokens per workgroup; the other 256 / (UN << tt_log2) threads take other heads.
 template <bool INTERLEAVED, int UN>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryKernelArgs a, int tt_log2) {
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryKernelArgs a, int tt_log2, unsigned first) {
   constexpr int UN_LOG2 = UN == 8 ? 3 : 2, kBatch = 2;
   const int tid = threadIdx.x, u = tid & (UN - 1);
   const int tok = (tid >> UN_LOG2) & ((1 << tt_log2) - 1), lane_head = tid >> (UN_LOG2 + tt_log2), step = 256 >> (UN_LOG2 + tt_log2);
-  const long long row = ((long long)blockIdx.x << tt_log2) + tok;
+  const long long row = ((long long)(blockIdx.x + first) << tt_log2) + tok;
   if (row >= a.rows) return;
   const uint32_t b = a.by_L.div((uint32_t)row), t = (uint32_t)row - b * (uint32_t)a.L;
   const bool rotated = u < a.rot_units;
@@ -122,15 +122,15 @@ hipError_t launch_rotary(const RotaryArgs& r, hipStream_t st) {
   // (Ordinary instead of non-temporal loads and stores: 142 us with 16 tokens.)
   int tt_log2 = 0;
   while (tt_log2 < 4 && (a.heads * a.units << tt_log2) < 256) ++tt_log2;
-  const unsigned grid = (unsigned)((a.rows + (1 << tt_log2) - 1) >> tt_log2);
-  if (r.d == 128) {
-    if (r.interleaved) rotary_kernel<true, 8><<<grid, 256, 0, st>>>(a, tt_log2);
-    else rotary_kernel<false, 8><<<grid, 256, 0, st>>>(a, tt_log2);
-  } else {
-    if (r.interleaved) rotary_kernel<true, 4><<<grid, 256, 0, st>>>(a, tt_log2);
-    else rotary_kernel<false, 4><<<grid, 256, 0, st>>>(a, tt_log2);
-  }
-  return hipGetLastError();
+  return launch_in_pieces((a.rows + (1 << tt_log2) - 1) >> tt_log2, [&](unsigned first, unsigned grid) {
+    if (r.d == 128) {
+      if (r.interleaved) rotary_kernel<true, 8><<<grid, 256, 0, st>>>(a, tt_log2, first);
+      else rotary_kernel<false, 8><<<grid, 256, 0, st>>>(a, tt_log2, first);
+    } else {
+      if (r.interleaved) rotary_kernel<true, 4><<<grid, 256, 0, st>>>(a, tt_log2, first);
+      else rotary_kernel<false, 4><<<grid, 256, 0, st>>>(a, tt_log2, first);
+    }
+  });
 }
 
 }  // namespace tsa

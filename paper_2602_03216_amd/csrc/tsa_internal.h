@@ -57,6 +57,18 @@ struct FastDiv {
 #endif
 };
 
+// A launch has fewer than 2^32 threads along an axis, so a call of more than 2^23 workgroups of 256 is several launches: launch(first workgroup, how many).
+template <typename F>
+hipError_t launch_in_pieces(long long blocks, F&& launch) {
+  constexpr long long most = 1ll << 23;
+  hipError_t e = hipSuccess;
+  for (long long first = 0; first < blocks && e == hipSuccess; first += most) {
+    launch((unsigned)first, (unsigned)(blocks - first < most ? blocks - first : most));
+    e = hipGetLastError();
+  }
+  return e;
+}
+
 // ---- launchers (each returns hipGetLastError() after queuing its kernels) ----
 
 // score.hip
