@@ -288,8 +288,8 @@ int tsa_sparse_layers(const float* drift, int32_t n_layers, double delta, int32_
  * Row (b, h, t) at position p = positions[b * L + t] (device int32 [B,L], any value), or start + t where positions is
  * NULL; the pair (x, y) of its columns that belongs to freq[i] becomes
  *   gain * (x cos a - y sin a, x sin a + y cos a),  a = p * freq[i],   i = 0 .. rot / 2 - 1.
- * Columns rot .. d - 1 are copied.  bf16 in and out, fp32 arithmetic, one rounding; angles are exact to 2^-32 of a turn
- * at every position.  A packed batch of sequences is B = 1, L = all tokens, with positions. */
+ * Columns rot .. d - 1 are copied.  bf16 in and out, fp32 arithmetic, one rounding; the angle, reduced to one turn before it becomes
+ * a float, is within 2^-25 of a turn at every position (|freq| <= 2 pi).  A packed batch of sequences is B = 1, L = all tokens, with positions. */
 #define TSA_ROTARY_MAX_FREQS 64
 typedef struct tsa_rotary_desc {
   int32_t B, Hq, Hkv, L;    /* as in tsa_desc; L = 0: nothing to do */
@@ -373,7 +373,7 @@ int tsa_cache_write(const tsa_cache_desc* desc, const void* K, const void* V, co
                     const int32_t* page_table, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream);
 
 /* Reads the first L positions of every sequence back: K, V [n_seqs,Hkv,L,d] bf16 out, every element written (zeros from position
- * kv_len[i] on), exactly the values the cache stands for.  What tsa_score, tsa_forward or tsa_attend can go on with. */
+ * kv_len[i] on), exactly the values the cache stands for where bf16 has them (8 bits under the smallest powers of two: to nearest even).  What tsa_score, tsa_forward or tsa_attend can go on with. */
 int tsa_cache_read(const tsa_cache_desc* desc, const void* k_pages, const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales,
                    const int32_t* kv_len, const int32_t* page_table, int32_t L, void* K, void* V, void* stream);
 

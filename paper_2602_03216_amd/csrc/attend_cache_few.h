@@ -5,7 +5,7 @@
 // the group, so K and V are read once for all of them.
 //
 // Few rows per sequence (single tokens, drafted tokens): K and V are what has to be read, HBM bounds it, and the keys are the axis that
-// fills the chip.  The work of the whole batch, counted in steps of 128 keys of one (sequence, KV head, tile of 16 rows), is cut into
+// fills the chip.  The work of the whole batch, counted in steps of 128 keys of one (sequence, KV head, tile of 16, 32 or 64 rows), is cut into
 // equal shares, one per workgroup; lengths are known on the device only, so every workgroup sums them up itself and finds its
 // place.  A share that covers only a part of a row tile's keys leaves its running max, sum and output in the workspace, and a second launch
 // joins them; whole ones are written at once.  Where contexts are short and few, a workgroup takes a whole tile instead (WHOLE).
@@ -59,6 +59,7 @@ __device__ __forceinline__ Seq one_sequence(const Args& a, int i, int rt, int st
 // Shares per CU, all of which run at once.  What they have in flight together is what the memory rate comes from: the rows of d = 64 in 8 bits
 // are short and take four (300 sequences x 1000 keys, 8 KV heads: 83 us with two, 70 with four, 6 x 131072 153 and 138); with longer rows two have enough
 // in flight, and more only cut the work finer (64 x 8192 in 8 bits, d = 128: 176 us with two, 189 with three; bf16, d = 64: 170 with two, 176 with four).
+// (In the joint launch with prompts two workgroups a CU run at once whatever this says: d = 64 in 8 bits has its shares there in two rounds, in the launch's tail.)
 constexpr int per_cu(int d, bool e4m3, int mb) { return mb == 4 && d == 128 ? 1 : mb == 1 && d == 64 && e4m3 ? 4 : 2; }
 
 template <int D, bool E4M3, int MB, int NW = 4>

@@ -5,7 +5,7 @@
 // Angles.  A position of a million times a frequency of one radian leaves 32-bit floats some 0.06 rad, so the angle is never
 // formed in radians: the host hands each frequency over in turns per position as a 64-bit fraction (2^64 = one turn), the
 // product with the position wraps around modulo one turn by itself, exactly, and its top 32 bits are the angle to 2^-32 of a
-// turn.  sin and cos are those of the 32-bit library on half turns in [-1, 1].
+// turn, as a 32-bit float within 2^-25.  sin and cos are those of the 32-bit library on half turns in [-1, 1].
 //
 // A thread owns eight pairs (two 16-byte pieces of a row: one from either half, or 32 consecutive bytes where the pairs
 // lie side by side) of one token, and takes them through the heads: sines and cosines are formed once per token, not once per
