@@ -80,7 +80,8 @@ class tsa_cache_desc(ctypes.Structure):
 
 def make_cache_desc(n_seqs, n_tokens, Hq, Hkv, d, page_size, n_pages, max_pages, format=TSA_CACHE_BF16, max_q=0, window=0, scale=0.0,
                     q_strides=(0, 0), k_strides=(0, 0), v_strides=(0, 0), o_strides=(0, 0)):
-    """*_strides = (stride of a token, stride of a head) in elements of the packed tensors; zeros = contiguous [n_tokens, heads, d]."""
+    """*_strides = (stride of a token, stride of a head) in elements of the packed tensors; zeros = contiguous [n_tokens, heads, d].
+    max_q: most new tokens of a sequence; 0 (not known) is right for any, and prepares the attention and its workspace for prompts."""
     return tsa_cache_desc(n_seqs, n_tokens, max_q, Hq, Hkv, d, page_size, n_pages, max_pages, format, window, scale,
                           *q_strides, *k_strides, *v_strides, *o_strides)
 
